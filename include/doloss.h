@@ -360,6 +360,120 @@ do_status do_rem_dispatch(const do_rem_move* replicas, const int32_t* n_replicas
                           hipStream_t stream);
 
 /*
+ * The chosen experts' products
+ * ----------------------------
+ * A token of the signatures is one row for each of its experts.  Rows are
+ * ordered by expert and then by token: expert e has rows offsets[e] ..
+ * offsets[e + 1] - 1, R = N k at most.  The operators below compute a gated
+ * expert layer y_t = sum_e p_te W2_e (silu(g) u), (g, u) = W1_e x_t, and its
+ * gradients, row by row.  `dtype` is the type of activations and weights
+ * (DO_F32 or DO_BF16); products, sums and activations are computed in fp32 and
+ * rounded once (to nearest even) where they are stored.  Row counts are read
+ * on the device: no call waits.
+ *   Rows past offsets[E] are neither read nor written.  Token indices are
+ *   clamped to [0, N), offsets to [0, R].
+ *   Limits: 1 <= E <= 1024, N and R in [1, 2^31), widths in [1, 65536]
+ *   (DO_ERR_OVERFLOW where a tile list would pass 2^31).  Any width and
+ *   element alignment is accepted; rows of whole 16-byte pieces at 16-byte
+ *   aligned addresses take the fast path.
+ */
+
+/*
+ * Rows of the experts from the signatures of one layer.
+ *   bits          [U][E][8] device (signature layout; bits past N are ignored)
+ *   offsets       [E + 1] device, overwritten
+ *   row_token     [N k] device: the token of row r, for r < offsets[E]
+ *   token_row     [N][k] device: a token's rows, in ascending order of their
+ *                 experts; -1 where a token has fewer than k experts
+ *   token_expert  [N][k] device: the experts of those rows; -1 likewise
+ *   workspace     device, 4-byte aligned, do_expert_rows_workspace(N, E) bytes
+ *                 at least (0 up to 512 tokens: then NULL is accepted)
+ * A token's experts past the k-th in ascending order get no row.
+ * Limits: N * k < 2^31 (DO_ERR_OVERFLOW).  Exact and deterministic.
+ */
+int64_t do_expert_rows_workspace(int64_t N, int32_t E);
+do_status do_expert_rows(const uint64_t* bits, int64_t N, int32_t E, int32_t k, int32_t* offsets, int32_t* row_token,
+                         int32_t* token_row, int32_t* token_expert, void* workspace, int64_t workspace_bytes,
+                         hipStream_t stream);
+
+/*
+ * Sum of the rows of each token: y_t = sum_j o[token_row[t][j]], in the order
+ * of j, in fp32; entries outside [0, N k) (such as -1) add nothing.
+ *   o  [N k][H] device;  y  [N][H] device, overwritten
+ */
+do_status do_expert_combine(const void* o, do_dtype dtype, const int32_t* token_row, int64_t N, int32_t k, int32_t H,
+                            void* y, hipStream_t stream);
+
+/*
+ * Products of the rows with their expert's weights.
+ *   transposed 0:  y_r [O] = W_e x_r,    x [R][I]
+ *   transposed 1:  y_r [I] = W_e^T x_r,  x [R][O]  (the gradient of the rows)
+ *   w          [E][O][I] device
+ *   row_token  nullable, device: row r is then x[row_token[r]], x [N][..]
+ */
+do_status do_expert_matmul(const void* x, const void* w, do_dtype dtype, const int32_t* offsets,
+                           const int32_t* row_token, int64_t N, int64_t R, int32_t E, int32_t O, int32_t I,
+                           int32_t transposed, void* y, hipStream_t stream);
+
+/*
+ * Gradients of the experts' weights: dW_e [O][I] = sum over e's rows of
+ * dy_r x_r^T, in fp32; zero for an expert without rows.
+ *   dy        [R][O] device, or [N][O] with dy_token (nullable, device)
+ *   x         [R][I] device, or [N][I] with x_token (nullable, device)
+ *   accumulate  not 0: added to what dw holds (gradient accumulation)
+ *   dw        [E][O][I] device
+ */
+do_status do_expert_weight_grad(const void* dy, const void* x, do_dtype dtype, const int32_t* offsets,
+                                const int32_t* dy_token, const int32_t* x_token, int64_t N, int64_t R, int32_t E,
+                                int32_t O, int32_t I, int32_t accumulate, float* dw, hipStream_t stream);
+
+/*
+ * First product and gated activation: (g, u) = W1_e x_t, g the first F of the
+ * 2 F rows of W1_e, and h_r = p_te silu(g) u for row r of token t and expert e.
+ *   x          [N][H] device, rows taken by row_token
+ *   w1         [E][2 F][H] device
+ *   p          nullable, [N][E] device of p_dtype: routing probabilities
+ *   h          [R][F] device, overwritten
+ *   q, e       nullable together: the checkpoint for the backward pass, g and u
+ *              in 8 bits (do_act8_pack), [R][2][F] and [R][2][ceil(F / 32)]
+ */
+do_status do_expert_swiglu(const void* x, const void* w1, do_dtype dtype, const void* p, do_dtype p_dtype,
+                           const int32_t* offsets, const int32_t* row_token, int64_t N, int64_t R, int32_t E,
+                           int32_t H, int32_t F, void* h, int8_t* q, uint8_t* e, hipStream_t stream);
+
+/*
+ * Backward pass of the gated activation and the second product, with g and u
+ * read from their 8-bit checkpoint (R = N k rows).  With dh_r = W2_e^T dy_t and
+ * s = silu(g) u:
+ *   da  [R][2 F] device: p_te dh u silu'(g), then p_te dh silu(g)
+ *   h   [R][F] device: p_te s again (what do_expert_weight_grad needs for W2)
+ *   dp  nullable, [N][E] device of p_dtype: sum_f dh s; 0 where t has no row
+ * dy is [N][H], w2 [E][H][F].  With dp, token_row, token_expert and a
+ * workspace of do_expert_swiglu_grad_workspace(N k, F) bytes are needed; else
+ * they may be NULL.  Deterministic.
+ */
+int64_t do_expert_swiglu_grad_workspace(int64_t R, int32_t F);
+do_status do_expert_swiglu_grad(const void* dy, const void* w2, do_dtype dtype, const void* p, do_dtype p_dtype,
+                                const int32_t* offsets, const int32_t* row_token, const int32_t* token_row,
+                                const int32_t* token_expert, int64_t N, int32_t E, int32_t k, int32_t H, int32_t F,
+                                const int8_t* q, const uint8_t* e, void* da, void* h, void* dp, void* workspace,
+                                int64_t workspace_bytes, hipStream_t stream);
+
+/*
+ * Activations in 8 bits.  32 consecutive elements of a row (the last group of
+ * a row may be shorter) share an exponent: the smallest e >= -126 with
+ * |x| <= 127 * 2^e for all of them, stored as e + 127, and each is
+ * q = x 2^-e rounded to the nearest integer, ties to even.  A group with an
+ * infinity or NaN is stored as 255 and reads back as NaN.
+ *   x  [rows][W];  q  [rows][W];  e  [rows][ceil(W / 32)], all device
+ * do_act8_unpack writes q 2^e, which is exact in fp32 and in bf16.
+ */
+do_status do_act8_pack(const void* x, do_dtype dtype, int64_t rows, int32_t W, int8_t* q, uint8_t* e,
+                       hipStream_t stream);
+do_status do_act8_unpack(const int8_t* q, const uint8_t* e, int64_t rows, int32_t W, void* x, do_dtype dtype,
+                         hipStream_t stream);
+
+/*
  * Process-wide options (they take effect at the next call; calls already
  * enqueued are unaffected).  Returns DO_ERR_INVALID_ARG for an unknown option
  * or a value out of range.  The first two override internal choices that

@@ -15,6 +15,9 @@ Functions keep the C names:
 * ``do_surrogate(p, k, bits, D)``    -> (loss [L] float64, dloss/dp [L][N][E] float32)
 * ``DoStream``                       -> streaming history (do_stream_*)
 * ``do_rem_allocate`` / ``do_rem_dispatch`` -> REM replica placement and token routes
+* ``do_expert_rows`` -> ExpertRows, and the chosen experts' products on them: ``do_expert_swiglu`` /
+  ``do_expert_swiglu_grad``, ``do_expert_matmul``, ``do_expert_weight_grad``, ``do_expert_combine``
+* ``do_act8_pack`` / ``do_act8_unpack`` -> activations in 8 bits (Act8) and back
 
 ``scores`` is a CUDA tensor of shape [N, E] or [L, N, E], float32 or bfloat16.
 """
@@ -23,6 +26,7 @@ from __future__ import annotations
 import array
 import ctypes
 import os
+from typing import NamedTuple
 
 import torch
 
@@ -77,6 +81,17 @@ def lib():
             "do_profile_next": ([vp, vp], st),
             "do_set_option": ([st, i32], st),
             "do_global_batch_noalloc": ([ctypes.POINTER(vp), st, i64, i32, i32, i32, vp, vp, vp, vp], st),
+            "do_expert_rows_workspace": ([i64, i32], i64),
+            "do_expert_rows": ([vp, i64, i32, i32, vp, vp, vp, vp, vp, i64, vp], st),
+            "do_expert_combine": ([vp, st, vp, i64, i32, i32, vp, vp], st),
+            "do_expert_matmul": ([vp, vp, st, vp, vp, i64, i64, i32, i32, i32, i32, vp, vp], st),
+            "do_expert_weight_grad": ([vp, vp, st, vp, vp, vp, i64, i64, i32, i32, i32, i32, vp, vp], st),
+            "do_expert_swiglu": ([vp, vp, st, vp, st, vp, vp, i64, i64, i32, i32, i32, vp, vp, vp, vp], st),
+            "do_expert_swiglu_grad_workspace": ([i64, i32], i64),
+            "do_expert_swiglu_grad": ([vp, vp, st, vp, st, vp, vp, vp, vp, i64, i32, i32, i32, i32, vp, vp, vp, vp, vp,
+                                       vp, i64, vp], st),
+            "do_act8_pack": ([vp, st, i64, i32, vp, vp, vp], st),
+            "do_act8_unpack": ([vp, vp, i64, i32, vp, st, vp], st),
             "do_rem_allocate": ([vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp, vp], st),
             "do_rem_dispatch": ([vp, vp, i32, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp, vp], st),
         }
@@ -539,3 +554,223 @@ class DoStream:
             self.close()
         except Exception:
             pass
+
+
+class ExpertRows(NamedTuple):
+    """Rows of the experts (do_expert_rows): offsets int32 [E + 1], row_token int32 [N k],
+    token_row and token_expert int32 [N, k]."""
+
+    offsets: torch.Tensor
+    row_token: torch.Tensor
+    token_row: torch.Tensor
+    token_expert: torch.Tensor
+
+
+class Act8(NamedTuple):
+    """Activations in 8 bits (do_act8_pack): q int8 [..., W], e uint8 [..., ceil(W / 32)]."""
+
+    q: torch.Tensor
+    e: torch.Tensor
+
+
+ACT8_GROUP = 32
+
+
+def _row_sizes(rows: ExpertRows):
+    """(N, E, k, R) of a set of rows, after checking them."""
+    if not isinstance(rows, ExpertRows):
+        raise ValueError("rows must be an ExpertRows (do_expert_rows)")
+    _want(rows.token_row, "rows.token_row", dtypes=_I32)
+    if rows.token_row.dim() != 2 or rows.offsets.dim() != 1:
+        raise ValueError("rows.token_row must have shape [N, k] and rows.offsets shape [E + 1]")
+    N, k = rows.token_row.shape
+    _want(rows.offsets, "rows.offsets", dtypes=_I32)
+    _want(rows.row_token, "rows.row_token", shape=(N * k,), dtypes=_I32)
+    _want(rows.token_expert, "rows.token_expert", shape=(N, k), dtypes=_I32)
+    return N, rows.offsets.shape[0] - 1, k, N * k
+
+
+def _out(t: torch.Tensor | None, name: str, shape, dtype, device) -> torch.Tensor:
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    _want(t, name, shape=shape, dtypes=(dtype,))
+    return t
+
+
+def do_expert_rows(bits: torch.Tensor, N: int, k: int) -> ExpertRows:
+    """Rows by expert of the signatures `bits` [U, E, 8] or [1, U, E, 8] of N tokens."""
+    if not isinstance(bits, torch.Tensor) or bits.dim() not in (3, 4) or bits.shape[-1] != 8:
+        raise ValueError("bits must be a tensor of shape [U, E, 8] or [1, U, E, 8]")
+    if bits.dim() == 4:
+        if bits.shape[0] != 1:
+            raise ValueError("do_expert_rows takes one layer: index bits first")
+        bits = bits[0]
+    U, E = bits.shape[0], bits.shape[1]
+    if U != _units(N):
+        raise ValueError(f"bits has {U} units, ceil(N/512) = {_units(N)} for N = {N}")
+    _want(bits, "bits", dtypes=_I64)
+    if not 1 <= k <= E:
+        raise ValueError(f"k = {k} must be in [1, E = {E}]")
+    dev = bits.device
+    rows = ExpertRows(torch.empty(E + 1, dtype=torch.int32, device=dev),
+                      torch.empty(N * k, dtype=torch.int32, device=dev),
+                      torch.empty((N, k), dtype=torch.int32, device=dev),
+                      torch.empty((N, k), dtype=torch.int32, device=dev))
+    need = lib().do_expert_rows_workspace(N, E)
+    ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    _check(lib().do_expert_rows(bits.data_ptr(), N, E, k, rows.offsets.data_ptr(), rows.row_token.data_ptr(),
+                                rows.token_row.data_ptr(), rows.token_expert.data_ptr(),
+                                ws.data_ptr() if ws is not None else None, need, _stream()), "do_expert_rows")
+    return rows
+
+
+def do_expert_combine(o: torch.Tensor, rows: ExpertRows, out: torch.Tensor | None = None) -> torch.Tensor:
+    """y [N, H]: the sum of each token's rows of `o` [N k, H]."""
+    N, E, k, R = _row_sizes(rows)
+    if not isinstance(o, torch.Tensor) or o.dim() != 2 or o.shape[0] != R:
+        raise ValueError(f"o must be a tensor of shape [{R}, H]")
+    _want(o, "o", dtypes=_SCORE_DTYPES)
+    H = o.shape[1]
+    y = _out(out, "out", (N, H), o.dtype, o.device)
+    _check(lib().do_expert_combine(o.data_ptr(), _dtype_code(o), rows.token_row.data_ptr(), N, k, H, y.data_ptr(),
+                                   _stream()), "do_expert_combine")
+    return y
+
+
+def _operand(t: torch.Tensor, name: str, shape, like: torch.Tensor | None = None):
+    if not isinstance(t, torch.Tensor) or tuple(t.shape) != shape:
+        raise ValueError(f"{name} must be a tensor of shape {list(shape)}")
+    _want(t, name, dtypes=_SCORE_DTYPES if like is None else (like.dtype,))
+
+
+def do_expert_matmul(x: torch.Tensor, w: torch.Tensor, rows: ExpertRows, gather: bool = False,
+                     transposed: bool = False, out: torch.Tensor | None = None) -> torch.Tensor:
+    """y [R, O] = W_e x_r for the weights w [E, O, I] and rows x [R, I]; transposed: y [R, I] = W_e^T x_r
+    for x [R, O].  gather: x holds the tokens ([N, ..]) and row r is x[row_token[r]]."""
+    N, E, k, R = _row_sizes(rows)
+    if not isinstance(w, torch.Tensor) or w.dim() != 3 or w.shape[0] != E:
+        raise ValueError(f"w must be a tensor of shape [{E}, O, I]")
+    _want(w, "w", dtypes=_SCORE_DTYPES)
+    O, I = w.shape[1], w.shape[2]
+    _operand(x, "x", (N if gather else R, O if transposed else I), w)
+    y = _out(out, "out", (R, I if transposed else O), w.dtype, w.device)
+    _check(lib().do_expert_matmul(x.data_ptr(), w.data_ptr(), _dtype_code(w), rows.offsets.data_ptr(),
+                                  rows.row_token.data_ptr() if gather else None, N, R, E, O, I, int(transposed),
+                                  y.data_ptr(), _stream()), "do_expert_matmul")
+    return y
+
+
+def do_expert_weight_grad(dy: torch.Tensor, x: torch.Tensor, rows: ExpertRows, gather_dy: bool = False,
+                          gather_x: bool = False, out: torch.Tensor | None = None,
+                          accumulate: bool = False) -> torch.Tensor:
+    """dW float32 [E, O, I] = sum over an expert's rows of dy_r x_r^T, for dy [R, O] and x [R, I]
+    (gather_dy, gather_x: [N, ..], taken by token).  accumulate: added to `out`."""
+    N, E, k, R = _row_sizes(rows)
+    if not isinstance(dy, torch.Tensor) or dy.dim() != 2 or not isinstance(x, torch.Tensor) or x.dim() != 2:
+        raise ValueError("dy and x must be tensors of shape [rows, O] and [rows, I]")
+    O, I = dy.shape[1], x.shape[1]
+    _operand(dy, "dy", (N if gather_dy else R, O))
+    _operand(x, "x", (N if gather_x else R, I), dy)
+    if accumulate and out is None:
+        raise ValueError("accumulate needs out")
+    dw = _out(out, "out", (E, O, I), torch.float32, dy.device)
+    tok = rows.row_token.data_ptr()
+    _check(lib().do_expert_weight_grad(dy.data_ptr(), x.data_ptr(), _dtype_code(dy), rows.offsets.data_ptr(),
+                                       tok if gather_dy else None, tok if gather_x else None, N, R, E, O, I,
+                                       int(accumulate), dw.data_ptr(), _stream()), "do_expert_weight_grad")
+    return dw
+
+
+def _probs_of(p: torch.Tensor | None, N: int, E: int):
+    if p is None:
+        return None, DO_F32
+    _want(p, "p", shape=(N, E), dtypes=_SCORE_DTYPES)
+    return p.data_ptr(), _dtype_code(p)
+
+
+def do_expert_swiglu(x: torch.Tensor, w1: torch.Tensor, rows: ExpertRows, p: torch.Tensor | None = None,
+                     checkpoint: bool = False):
+    """(h [R, F], checkpoint): h_r = p_te silu(g) u with (g, u) = W1_e x_t, for tokens x [N, H], weights
+    w1 [E, 2 F, H] (gate rows, then up rows) and probabilities p [N, E] or None (1).  checkpoint: g and u in
+    8 bits (an Act8 of [R, 2, F]) for do_expert_swiglu_grad; else None is returned in its place."""
+    N, E, k, R = _row_sizes(rows)
+    if not isinstance(w1, torch.Tensor) or w1.dim() != 3 or w1.shape[0] != E or w1.shape[1] % 2:
+        raise ValueError(f"w1 must be a tensor of shape [{E}, 2 F, H]")
+    _want(w1, "w1", dtypes=_SCORE_DTYPES)
+    F, H = w1.shape[1] // 2, w1.shape[2]
+    _operand(x, "x", (N, H), w1)
+    pp, pd = _probs_of(p, N, E)
+    dev = w1.device
+    h = torch.empty((R, F), dtype=w1.dtype, device=dev)
+    kept = None
+    if checkpoint:
+        kept = Act8(torch.empty((R, 2, F), dtype=torch.int8, device=dev),
+                    torch.empty((R, 2, -(-F // ACT8_GROUP)), dtype=torch.uint8, device=dev))
+    _check(lib().do_expert_swiglu(x.data_ptr(), w1.data_ptr(), _dtype_code(w1), pp, pd, rows.offsets.data_ptr(),
+                                  rows.row_token.data_ptr(), N, R, E, H, F, h.data_ptr(),
+                                  kept.q.data_ptr() if kept else None, kept.e.data_ptr() if kept else None,
+                                  _stream()), "do_expert_swiglu")
+    return h, kept
+
+
+def do_expert_swiglu_grad(dy: torch.Tensor, w2: torch.Tensor, rows: ExpertRows, checkpoint: Act8,
+                          p: torch.Tensor | None = None):
+    """(da [R, 2 F], h [R, F], dp [N, E] or None) of do_expert_swiglu followed by the second product with
+    w2 [E, H, F] and the sum over a token's rows: dy [N, H] is the gradient of that sum, da that of (g, u),
+    dp that of p (in p's type; None without p), and h = p silu(g) u again, for the gradient of w2."""
+    N, E, k, R = _row_sizes(rows)
+    if not isinstance(w2, torch.Tensor) or w2.dim() != 3 or w2.shape[0] != E:
+        raise ValueError(f"w2 must be a tensor of shape [{E}, H, F]")
+    _want(w2, "w2", dtypes=_SCORE_DTYPES)
+    H, F = w2.shape[1], w2.shape[2]
+    _operand(dy, "dy", (N, H), w2)
+    if not isinstance(checkpoint, Act8):
+        raise ValueError("checkpoint must be an Act8 (do_expert_swiglu with checkpoint=True)")
+    _want(checkpoint.q, "checkpoint.q", shape=(R, 2, F), dtypes=(torch.int8,))
+    _want(checkpoint.e, "checkpoint.e", shape=(R, 2, -(-F // ACT8_GROUP)), dtypes=_U8)
+    pp, pd = _probs_of(p, N, E)
+    dev = w2.device
+    da = torch.empty((R, 2 * F), dtype=w2.dtype, device=dev)
+    h = torch.empty((R, F), dtype=w2.dtype, device=dev)
+    dp = ws = None
+    need = 0
+    if p is not None:
+        dp = torch.empty((N, E), dtype=p.dtype, device=dev)
+        need = lib().do_expert_swiglu_grad_workspace(R, F)
+        ws = torch.empty(need, dtype=torch.uint8, device=dev)
+    _check(lib().do_expert_swiglu_grad(dy.data_ptr(), w2.data_ptr(), _dtype_code(w2), pp, pd, rows.offsets.data_ptr(),
+                                       rows.row_token.data_ptr(), rows.token_row.data_ptr(),
+                                       rows.token_expert.data_ptr(), N, E, k, H, F, checkpoint.q.data_ptr(),
+                                       checkpoint.e.data_ptr(), da.data_ptr(), h.data_ptr(),
+                                       dp.data_ptr() if dp is not None else None,
+                                       ws.data_ptr() if ws is not None else None, need, _stream()),
+           "do_expert_swiglu_grad")
+    return da, h, dp
+
+
+def do_act8_pack(x: torch.Tensor) -> Act8:
+    """x [..., W] (float32 or bfloat16) in 8 bits, 32 elements of a row sharing an exponent."""
+    if not isinstance(x, torch.Tensor) or x.dim() < 1 or x.numel() == 0:
+        raise ValueError("x must be a tensor of shape [..., W] with at least one element")
+    _want(x, "x", dtypes=_SCORE_DTYPES)
+    W = x.shape[-1]
+    a = Act8(torch.empty(x.shape, dtype=torch.int8, device=x.device),
+             torch.empty((*x.shape[:-1], -(-W // ACT8_GROUP)), dtype=torch.uint8, device=x.device))
+    _check(lib().do_act8_pack(x.data_ptr(), _dtype_code(x), x.numel() // W, W, a.q.data_ptr(), a.e.data_ptr(),
+                              _stream()), "do_act8_pack")
+    return a
+
+
+def do_act8_unpack(a: Act8, dtype: torch.dtype, out: torch.Tensor | None = None) -> torch.Tensor:
+    """The values of an Act8 in float32 or bfloat16."""
+    if not isinstance(a, Act8) or a.q.dim() < 1 or a.q.numel() == 0:
+        raise ValueError("a must be an Act8 with at least one element")
+    if dtype not in _SCORE_DTYPES:
+        raise ValueError(f"dtype {dtype} is not one of {_SCORE_DTYPES}")
+    W = a.q.shape[-1]
+    _want(a.q, "q", dtypes=(torch.int8,))
+    _want(a.e, "e", shape=(*a.q.shape[:-1], -(-W // ACT8_GROUP)), dtypes=_U8)
+    x = _out(out, "out", tuple(a.q.shape), dtype, a.q.device)
+    _check(lib().do_act8_unpack(a.q.data_ptr(), a.e.data_ptr(), a.q.numel() // W, W, x.data_ptr(), _dtype_code(x),
+                                _stream()), "do_act8_unpack")
+    return x

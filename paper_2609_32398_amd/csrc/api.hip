@@ -7,7 +7,7 @@
 #include <new>
 #include <string>
 
-#include "common.h"
+#include "experts.h"
 
 #define DOLOSS_API extern "C" __attribute__((visibility("default")))
 
@@ -55,6 +55,12 @@ do_status hip_status(hipError_t e, const char* where) {
   g_last_error = std::string(where) + ": " + hipGetErrorString(e);
   return DO_ERR_HIP;
 }
+
+}  // namespace
+
+do_status dol::set_error(do_status st, const char* msg) { return fail(st, msg); }
+
+namespace {
 
 size_t dtype_size(do_dtype dt) { return dt == DO_F32 ? 4 : 2; }
 

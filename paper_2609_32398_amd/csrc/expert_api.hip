@@ -1,0 +1,290 @@
+// Host side of the experts' entry points declared in include/doloss.h:
+// argument validation and dispatch to the kernels.
+#include <algorithm>
+#include <initializer_list>
+
+#include "experts.h"
+
+#define DOLOSS_API extern "C" __attribute__((visibility("default")))
+
+using dol::set_error;
+using dol::u64;
+
+namespace {
+
+#define DO_TRY(expr)              \
+  do {                            \
+    const do_status st_ = (expr); \
+    if (st_ != DO_OK) return st_; \
+  } while (0)
+
+bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+
+do_status launched(hipError_t e) { return e == hipSuccess ? DO_OK : set_error(DO_ERR_HIP, hipGetErrorString(e)); }
+
+do_status check_dtype(int dt) {
+  if (dt != DO_F32 && dt != DO_BF16) return set_error(DO_ERR_UNSUPPORTED_DTYPE, "dtype must be DO_F32 or DO_BF16");
+  return DO_OK;
+}
+size_t size_of(do_dtype dt) { return dt == DO_F32 ? 4 : 2; }
+
+do_status check_ptr(const void* p, size_t align, const char* msg) {
+  return p == nullptr || !aligned(p, align) ? set_error(DO_ERR_INVALID_ARG, msg) : DO_OK;
+}
+
+do_status check_experts(int64_t N, int32_t E, int32_t k) {
+  if (E < 1 || E > dol::kMaxE) return set_error(DO_ERR_INVALID_ARG, "E must be in [1, 1024]");
+  if (k < 1 || k > E) return set_error(DO_ERR_INVALID_ARG, "k must be in [1, E]");
+  if (N < 1) return set_error(DO_ERR_INVALID_ARG, "N must be >= 1");
+  if (N >= (int64_t(1) << 31) || N * k >= (int64_t(1) << 31))
+    return set_error(DO_ERR_OVERFLOW, "N * k must be < 2^31 (rows are int32)");
+  return DO_OK;
+}
+do_status check_rows(int64_t N, int64_t R, int32_t E) {
+  if (E < 1 || E > dol::kMaxE) return set_error(DO_ERR_INVALID_ARG, "E must be in [1, 1024]");
+  if (N < 1 || R < 1) return set_error(DO_ERR_INVALID_ARG, "N and R must be >= 1");
+  if (N >= (int64_t(1) << 31) || R >= (int64_t(1) << 31))
+    return set_error(DO_ERR_OVERFLOW, "N and R must be < 2^31 (rows are int32)");
+  return DO_OK;
+}
+do_status check_widths(int64_t R, int32_t E, std::initializer_list<int32_t> w) {
+  int64_t tiles = 1;
+  for (int32_t v : w) {
+    if (v < 1 || v > dol::kMaxWidth) return set_error(DO_ERR_INVALID_ARG, "widths must be in [1, 65536]");
+    tiles = std::max<int64_t>(tiles, (v + 63) / 64);
+  }
+  // the tile list of a product is counted in int32
+  if ((R / 128 + E) * tiles >= (int64_t(1) << 31))
+    return set_error(DO_ERR_OVERFLOW, "too many rows for rows of this width");
+  return DO_OK;
+}
+// 16-byte pieces of an operand: its address and the length of its rows.
+bool whole(const void* p, do_dtype dt, int32_t row) { return aligned(p, 16) && row * size_of(dt) % 16 == 0; }
+
+}  // namespace
+
+DOLOSS_API int64_t do_expert_rows_workspace(int64_t N, int32_t E) {
+  if (N < 1 || E < 1 || E > dol::kMaxE) return 0;
+  const int64_t U = (N - 1) / 512 + 1;
+  return U == 1 ? 0 : std::min<int64_t>(U, dol::kRowChunks) * E * (int64_t)sizeof(uint32_t);
+}
+
+DOLOSS_API do_status do_expert_rows(const uint64_t* bits, int64_t N, int32_t E, int32_t k, int32_t* offsets,
+                                    int32_t* row_token, int32_t* token_row, int32_t* token_expert, void* workspace,
+                                    int64_t workspace_bytes, hipStream_t stream) {
+  DO_TRY(check_experts(N, E, k));
+  DO_TRY(check_ptr(bits, 8, "bits is NULL or not 8-byte aligned"));
+  DO_TRY(check_ptr(offsets, 4, "offsets is NULL or not 4-byte aligned"));
+  DO_TRY(check_ptr(row_token, 4, "row_token is NULL or not 4-byte aligned"));
+  DO_TRY(check_ptr(token_row, 4, "token_row is NULL or not 4-byte aligned"));
+  DO_TRY(check_ptr(token_expert, 4, "token_expert is NULL or not 4-byte aligned"));
+  const int64_t need = do_expert_rows_workspace(N, E);
+  if (need > 0) {
+    DO_TRY(check_ptr(workspace, 4, "workspace is NULL or not 4-byte aligned"));
+    if (workspace_bytes < need)
+      return set_error(DO_ERR_INVALID_ARG, "workspace is smaller than do_expert_rows_workspace(N, E)");
+  }
+  return launched(dol::launch_expert_rows(reinterpret_cast<const u64*>(bits), N, E, k, offsets, row_token, token_row,
+                                          token_expert, static_cast<uint32_t*>(workspace), stream));
+}
+
+DOLOSS_API do_status do_expert_combine(const void* o, do_dtype dtype, const int32_t* token_row, int64_t N, int32_t k,
+                                       int32_t H, void* y, hipStream_t stream) {
+  DO_TRY(check_dtype(dtype));
+  DO_TRY(check_experts(N, dol::kMaxE, k));
+  DO_TRY(check_widths(N, 1, {H}));
+  DO_TRY(check_ptr(o, size_of(dtype), "o is NULL or not aligned to its element size"));
+  DO_TRY(check_ptr(token_row, 4, "token_row is NULL or not 4-byte aligned"));
+  DO_TRY(check_ptr(y, size_of(dtype), "y is NULL or not aligned to its element size"));
+  return launched(dol::launch_expert_combine(o, dtype, token_row, N, k, N * k, H, y, stream));
+}
+
+DOLOSS_API do_status do_expert_matmul(const void* x, const void* w, do_dtype dtype, const int32_t* offsets,
+                                      const int32_t* row_token, int64_t N, int64_t R, int32_t E, int32_t O, int32_t I,
+                                      int32_t transposed, void* y, hipStream_t stream) {
+  DO_TRY(check_dtype(dtype));
+  DO_TRY(check_rows(N, R, E));
+  DO_TRY(check_widths(R, E, {O, I}));
+  DO_TRY(check_ptr(x, size_of(dtype), "x is NULL or not aligned to its element size"));
+  DO_TRY(check_ptr(w, size_of(dtype), "w is NULL or not aligned to its element size"));
+  DO_TRY(check_ptr(y, size_of(dtype), "y is NULL or not aligned to its element size"));
+  DO_TRY(check_ptr(offsets, 4, "offsets is NULL or not 4-byte aligned"));
+  if (row_token != nullptr && !aligned(row_token, 4))
+    return set_error(DO_ERR_INVALID_ARG, "row_token is not 4-byte aligned");
+  const int32_t in = transposed ? O : I, out = transposed ? I : O;
+  dol::ExpertGemm g{};
+  g.P = w;
+  g.Q = x;
+  g.offsets = offsets;
+  g.q_token = row_token;
+  g.N = N;
+  g.R = R;
+  g.E = E;
+  g.Pd = out;
+  g.K = in;
+  g.ldp = I;
+  g.ldq = in;
+  g.out = y;
+  g.vec_out = whole(y, dtype, out);
+  return launched(
+      dol::launch_expert_matmul(g, dtype, transposed != 0, whole(w, dtype, I) && whole(x, dtype, in), stream));
+}
+
+DOLOSS_API do_status do_expert_weight_grad(const void* dy, const void* x, do_dtype dtype, const int32_t* offsets,
+                                           const int32_t* dy_token, const int32_t* x_token, int64_t N, int64_t R,
+                                           int32_t E, int32_t O, int32_t I, int32_t accumulate, float* dw,
+                                           hipStream_t stream) {
+  DO_TRY(check_dtype(dtype));
+  DO_TRY(check_rows(N, R, E));
+  DO_TRY(check_widths(1, E, {O, I}));
+  DO_TRY(check_ptr(dy, size_of(dtype), "dy is NULL or not aligned to its element size"));
+  DO_TRY(check_ptr(x, size_of(dtype), "x is NULL or not aligned to its element size"));
+  DO_TRY(check_ptr(dw, 4, "dw is NULL or not 4-byte aligned"));
+  DO_TRY(check_ptr(offsets, 4, "offsets is NULL or not 4-byte aligned"));
+  if ((dy_token != nullptr && !aligned(dy_token, 4)) || (x_token != nullptr && !aligned(x_token, 4)))
+    return set_error(DO_ERR_INVALID_ARG, "dy_token / x_token is not 4-byte aligned");
+  if ((int64_t)E * ((O + 63) / 64) * ((I + 63) / 64) >= (int64_t(1) << 31))
+    return set_error(DO_ERR_OVERFLOW, "too many weights");
+  dol::ExpertGemm g{};
+  g.P = x;
+  g.Q = dy;
+  g.offsets = offsets;
+  g.p_token = x_token;
+  g.q_token = dy_token;
+  g.N = N;
+  g.R = R;
+  g.E = E;
+  g.Pd = I;
+  g.Qd = O;
+  g.ldp = I;
+  g.ldq = O;
+  g.accumulate = accumulate != 0;
+  g.out = dw;
+  g.vec_out = whole(dw, DO_F32, I);
+  return launched(dol::launch_expert_weight_grad(g, dtype, whole(x, dtype, I) && whole(dy, dtype, O), stream));
+}
+
+namespace {
+
+// What do_expert_swiglu and do_expert_swiglu_grad check alike.
+do_status check_swiglu(do_dtype dtype, const void* p, do_dtype p_dtype, const int32_t* offsets,
+                       const int32_t* row_token, int64_t N, int64_t R, int32_t E, int32_t H, int32_t F) {
+  DO_TRY(check_dtype(dtype));
+  DO_TRY(check_rows(N, R, E));
+  DO_TRY(check_widths(R, E, {H, F}));
+  if (p != nullptr) {
+    DO_TRY(check_dtype(p_dtype));
+    if (!aligned(p, size_of(p_dtype))) return set_error(DO_ERR_INVALID_ARG, "p is not aligned to its element size");
+  }
+  DO_TRY(check_ptr(offsets, 4, "offsets is NULL or not 4-byte aligned"));
+  return check_ptr(row_token, 4, "row_token is NULL or not 4-byte aligned");
+}
+
+}  // namespace
+
+DOLOSS_API do_status do_expert_swiglu(const void* x, const void* w1, do_dtype dtype, const void* p, do_dtype p_dtype,
+                                      const int32_t* offsets, const int32_t* row_token, int64_t N, int64_t R,
+                                      int32_t E, int32_t H, int32_t F, void* h, int8_t* q, uint8_t* e,
+                                      hipStream_t stream) {
+  DO_TRY(check_swiglu(dtype, p, p_dtype, offsets, row_token, N, R, E, H, F));
+  DO_TRY(check_ptr(x, size_of(dtype), "x is NULL or not aligned to its element size"));
+  DO_TRY(check_ptr(w1, size_of(dtype), "w1 is NULL or not aligned to its element size"));
+  DO_TRY(check_ptr(h, size_of(dtype), "h is NULL or not aligned to its element size"));
+  if ((q == nullptr) != (e == nullptr)) return set_error(DO_ERR_INVALID_ARG, "q and e are given together or not at all");
+  dol::ExpertGemm g{};
+  g.P = w1;
+  g.Q = x;
+  g.offsets = offsets;
+  g.q_token = row_token;
+  g.N = N;
+  g.R = R;
+  g.E = E;
+  g.Pd = F;
+  g.K = H;
+  g.ldp = H;
+  g.ldq = H;
+  g.prob = p;
+  g.p_bf16 = p_dtype == DO_BF16;
+  g.q8 = q;
+  g.e8 = e;
+  g.out = h;
+  g.vec_out = aligned(h, 16) && F % 8 == 0;
+  g.vec_q8 = q != nullptr && aligned(q, 8) && F % 8 == 0;
+  return launched(dol::launch_expert_swiglu(g, dtype, whole(x, dtype, H) && whole(w1, dtype, H), stream));
+}
+
+DOLOSS_API int64_t do_expert_swiglu_grad_workspace(int64_t R, int32_t F) {
+  return R < 1 || F < 1 ? 0 : R * ((F + 63) / 64) * (int64_t)sizeof(float);
+}
+
+DOLOSS_API do_status do_expert_swiglu_grad(const void* dy, const void* w2, do_dtype dtype, const void* p,
+                                           do_dtype p_dtype, const int32_t* offsets, const int32_t* row_token,
+                                           const int32_t* token_row, const int32_t* token_expert, int64_t N, int32_t E,
+                                           int32_t k, int32_t H, int32_t F, const int8_t* q, const uint8_t* e,
+                                           void* da, void* h, void* dp, void* workspace, int64_t workspace_bytes,
+                                           hipStream_t stream) {
+  DO_TRY(check_experts(N, E, k));
+  const int64_t R = N * k;
+  DO_TRY(check_swiglu(dtype, p, p_dtype, offsets, row_token, N, R, E, H, F));
+  DO_TRY(check_ptr(dy, size_of(dtype), "dy is NULL or not aligned to its element size"));
+  DO_TRY(check_ptr(w2, size_of(dtype), "w2 is NULL or not aligned to its element size"));
+  DO_TRY(check_ptr(da, size_of(dtype), "da is NULL or not aligned to its element size"));
+  DO_TRY(check_ptr(h, size_of(dtype), "h is NULL or not aligned to its element size"));
+  DO_TRY(check_ptr(q, 1, "q is NULL"));
+  DO_TRY(check_ptr(e, 1, "e is NULL"));
+  if (dp != nullptr) {
+    if (p == nullptr) return set_error(DO_ERR_INVALID_ARG, "dp is the gradient of p, which is NULL");
+    if (!aligned(dp, size_of(p_dtype))) return set_error(DO_ERR_INVALID_ARG, "dp is not aligned to its element size");
+    DO_TRY(check_ptr(token_row, 4, "token_row is NULL or not 4-byte aligned"));
+    DO_TRY(check_ptr(token_expert, 4, "token_expert is NULL or not 4-byte aligned"));
+    DO_TRY(check_ptr(workspace, 4, "workspace is NULL or not 4-byte aligned"));
+    if (workspace_bytes < do_expert_swiglu_grad_workspace(R, F))
+      return set_error(DO_ERR_INVALID_ARG, "workspace is smaller than do_expert_swiglu_grad_workspace(R, F)");
+  }
+  dol::ExpertGemm g{};
+  g.P = w2;
+  g.Q = dy;
+  g.offsets = offsets;
+  g.q_token = row_token;
+  g.N = N;
+  g.R = R;
+  g.E = E;
+  g.Pd = F;
+  g.K = H;
+  g.ldp = F;
+  g.ldq = H;
+  g.prob = p;
+  g.p_bf16 = p_dtype == DO_BF16;
+  g.q8 = const_cast<int8_t*>(q);
+  g.e8 = const_cast<uint8_t*>(e);
+  g.out = da;
+  g.out2 = h;
+  g.dp = dp != nullptr ? static_cast<float*>(workspace) : nullptr;
+  g.vec_out = aligned(da, 16) && aligned(h, 16) && F % 8 == 0;
+  g.vec_q8 = aligned(q, 8) && F % 8 == 0;
+  DO_TRY(launched(dol::launch_expert_swiglu_grad(g, dtype, whole(dy, dtype, H) && whole(w2, dtype, F), stream)));
+  if (dp == nullptr) return DO_OK;
+  return launched(dol::launch_expert_dp(g.dp, (F + 63) / 64, R, token_row, token_expert, N, k, E, dp, p_dtype, stream));
+}
+
+DOLOSS_API do_status do_act8_pack(const void* x, do_dtype dtype, int64_t rows, int32_t W, int8_t* q, uint8_t* e,
+                                  hipStream_t stream) {
+  DO_TRY(check_dtype(dtype));
+  DO_TRY(check_rows(1, rows, 1));
+  DO_TRY(check_widths(1, 1, {W}));
+  DO_TRY(check_ptr(x, size_of(dtype), "x is NULL or not aligned to its element size"));
+  DO_TRY(check_ptr(q, 1, "q is NULL"));
+  DO_TRY(check_ptr(e, 1, "e is NULL"));
+  return launched(dol::launch_act8_pack(x, dtype, rows, W, q, e, stream));
+}
+
+DOLOSS_API do_status do_act8_unpack(const int8_t* q, const uint8_t* e, int64_t rows, int32_t W, void* x,
+                                    do_dtype dtype, hipStream_t stream) {
+  DO_TRY(check_dtype(dtype));
+  DO_TRY(check_rows(1, rows, 1));
+  DO_TRY(check_widths(1, 1, {W}));
+  DO_TRY(check_ptr(q, 1, "q is NULL"));
+  DO_TRY(check_ptr(e, 1, "e is NULL"));
+  DO_TRY(check_ptr(x, size_of(dtype), "x is NULL or not aligned to its element size"));
+  return launched(dol::launch_act8_unpack(q, e, rows, W, x, dtype, stream));
+}
