@@ -58,8 +58,13 @@ do_status check_widths(int64_t R, int32_t E, std::initializer_list<int32_t> w) {
     return set_error(DO_ERR_OVERFLOW, "too many rows for rows of this width");
   return DO_OK;
 }
-// 16-byte pieces of an operand: its address and the length of its rows.
-bool whole(const void* p, do_dtype dt, int32_t row) { return aligned(p, 16) && row * size_of(dt) % 16 == 0; }
+// An operand of whole 16-byte pieces: its address and the length of its rows, and fewer than 2^32 pieces.
+bool whole(const void* p, do_dtype dt, int32_t row, int64_t rows = 1) {
+  return aligned(p, 16) && row * size_of(dt) % 16 == 0 && rows * (int64_t)(row * size_of(dt) / 16) < (int64_t(1) << 32);
+}
+
+// Rows taken by token whose byte offsets pass 32 bits.
+int32_t wide(do_dtype dt, int32_t row, int64_t rows) { return rows * row * (int64_t)size_of(dt) >= (int64_t(1) << 32); }
 
 }  // namespace
 
@@ -125,9 +130,10 @@ DOLOSS_API do_status do_expert_matmul(const void* x, const void* w, do_dtype dty
   g.ldp = I;
   g.ldq = in;
   g.out = y;
+  g.wide = row_token != nullptr && wide(dtype, in, N);
   g.vec_out = whole(y, dtype, out);
   return launched(
-      dol::launch_expert_matmul(g, dtype, transposed != 0, whole(w, dtype, I) && whole(x, dtype, in), stream));
+      dol::launch_expert_matmul(g, dtype, transposed != 0, whole(w, dtype, I) && whole(x, dtype, in, row_token != nullptr ? N : R), stream));
 }
 
 DOLOSS_API do_status do_expert_weight_grad(const void* dy, const void* x, do_dtype dtype, const int32_t* offsets,
@@ -160,8 +166,12 @@ DOLOSS_API do_status do_expert_weight_grad(const void* dy, const void* x, do_dty
   g.ldq = O;
   g.accumulate = accumulate != 0;
   g.out = dw;
+  g.wide = wide(dtype, std::max(O, I), N);
   g.vec_out = whole(dw, DO_F32, I);
-  return launched(dol::launch_expert_weight_grad(g, dtype, whole(x, dtype, I) && whole(dy, dtype, O), stream));
+  // large tiles where there are enough of them for every CU
+  const bool big = I > 128 && O > 64 && (int64_t)E * I * O >= int64_t(256) * 65536;
+  return launched((dtype == DO_F32 ? dol::launch_expert_weight_grad_f32 : dol::launch_expert_weight_grad_bf16)(
+      g, big, whole(x, dtype, I, std::max(N, R)) && whole(dy, dtype, O, std::max(N, R)), stream));
 }
 
 namespace {
@@ -203,6 +213,7 @@ DOLOSS_API do_status do_expert_swiglu(const void* x, const void* w1, do_dtype dt
   g.K = H;
   g.ldp = H;
   g.ldq = H;
+  g.wide = wide(dtype, H, N);
   g.prob = p;
   g.p_bf16 = p_dtype == DO_BF16;
   g.q8 = q;
@@ -210,7 +221,7 @@ DOLOSS_API do_status do_expert_swiglu(const void* x, const void* w1, do_dtype dt
   g.out = h;
   g.vec_out = aligned(h, 16) && F % 8 == 0;
   g.vec_q8 = q != nullptr && aligned(q, 8) && F % 8 == 0;
-  return launched(dol::launch_expert_swiglu(g, dtype, whole(x, dtype, H) && whole(w1, dtype, H), stream));
+  return launched(dol::launch_expert_swiglu(g, dtype, whole(x, dtype, H, N) && whole(w1, dtype, H), stream));
 }
 
 DOLOSS_API int64_t do_expert_swiglu_grad_workspace(int64_t R, int32_t F) {
@@ -253,6 +264,7 @@ DOLOSS_API do_status do_expert_swiglu_grad(const void* dy, const void* w2, do_dt
   g.K = H;
   g.ldp = F;
   g.ldq = H;
+  g.wide = wide(dtype, H, N);
   g.prob = p;
   g.p_bf16 = p_dtype == DO_BF16;
   g.q8 = const_cast<int8_t*>(q);
@@ -262,7 +274,7 @@ DOLOSS_API do_status do_expert_swiglu_grad(const void* dy, const void* w2, do_dt
   g.dp = dp != nullptr ? static_cast<float*>(workspace) : nullptr;
   g.vec_out = aligned(da, 16) && aligned(h, 16) && F % 8 == 0;
   g.vec_q8 = aligned(q, 8) && F % 8 == 0;
-  DO_TRY(launched(dol::launch_expert_swiglu_grad(g, dtype, whole(dy, dtype, H) && whole(w2, dtype, F), stream)));
+  DO_TRY(launched(dol::launch_expert_swiglu_grad(g, dtype, whole(dy, dtype, H, N) && whole(w2, dtype, F), stream)));
   if (dp == nullptr) return DO_OK;
   return launched(dol::launch_expert_dp(g.dp, (F + 63) / 64, R, token_row, token_expert, N, k, E, dp, p_dtype, stream));
 }

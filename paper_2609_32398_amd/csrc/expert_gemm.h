@@ -16,12 +16,18 @@
 // tiles.  The experts' row counts are read on the device.
 //
 // A stage is 128 bytes of k for an operand row (k inner), or that many rows of k
-// (k outer), in LDS, double buffered: while a stage is multiplied the next one
-// is loaded, across tiles too.  A 16-byte piece of a stage lies at a place
-// XOR-ed with its row, so that the matrix operands are read from LDS without
-// bank conflicts; the loads that go straight to LDS write it in lane order, so
-// it is the global address of each lane that is permuted.
+// (k outer), in LDS, double buffered: while a stage is multiplied the next one is
+// loaded, across tiles too.  Half of the waves, one on each SIMD, issue all loads
+// of a stage: the vector cache holds no more than 32 KiB on their way, so that
+// the issue of a stage's 64 KiB takes about half of its time, in which the other
+// wave of the SIMD multiplies.
+// A 16-byte piece of a stage lies at a place XOR-ed with its row, so that the
+// matrix operands are read from LDS without bank conflicts; the loads that go
+// straight to LDS write it in lane order, so it is the global address of each
+// lane that is permuted.
 #pragma once
+
+#include <type_traits>
 
 #include "experts.h"
 
@@ -37,23 +43,27 @@ typedef short v4s __attribute__((ext_vector_type(4)));
 #define DOL_LDS __attribute__((address_space(3)))
 
 enum { kInner = 0, kOuter = 1 };  // where the contraction lies in an operand's rows
+enum { kElements = 0, kPieces = 1, kWidePieces = 2 };  // how the operands are loaded
 enum { kStore = 0, kWeightGrad = 1, kSwiglu = 2, kSwigluGrad = 3 };
 
 constexpr int kStageBytes = 128;  // of k for one operand row
+constexpr int kList = 1024;       // tokens of a list in LDS
+constexpr int kPhases = 4;        // of a stage: a quarter of its k each
 
-// Tile of BP x BQ outputs by WP x WQ waves, each 64 x (BQ / WQ).
+// Tile of BP x BQ outputs by WP x WQ waves.
 template <int BP_, int BQ_, int WP_, int WQ_, int OCC_>
 struct Tile {
   static constexpr int BP = BP_, BQ = BQ_, WP = WP_, WQ = WQ_;
   static constexpr int waves = WP * WQ, threads = waves * kWave;
+  static constexpr int loaders = threads / 2;                 // threads that load
   static constexpr int MP = BP / WP / 32, MQ = BQ / WQ / 32;  // 32 x 32 matrix tiles of a wave
   static constexpr int stage = (BP + BQ) * kStageBytes;
   static constexpr int occ = OCC_;  // waves per SIMD to leave registers for
-  static_assert(MP == 2, "a wave's outputs are 64 wide: a gate and an up tile, or 128 bytes of bf16");
-  static_assert(stage / waves >= 8192, "the epilogue's staging area of a wave");
+  static_assert(MP % 2 == 0, "a wave's outputs go out 64 wide: a gate and an up tile, or 128 bytes of bf16");
+  static_assert(stage / waves >= 4096, "the area of a wave's outputs on their way out");
 };
 using Big = Tile<256, 256, 4, 2, 2>;
-using Small = Tile<128, 128, 2, 2, 2>;
+using Small = Tile<128, 64, 2, 2, 2>;
 
 template <typename T>
 struct Mma;
@@ -77,137 +87,269 @@ struct Mma<float> {
   }
 };
 
-// Source of the pieces that lie past an operand's end.
-static __device__ const v4u zero_piece = {0u, 0u, 0u, 0u};
-
+// 16 bytes per lane from base (uniform) + off straight to LDS, lane after lane
+// from byte address lds + place (uniform).  The statements name no memory: the
+// place written is in a stage that no wave reads before a later wave_barrier,
+// and volatile statements keep their order.
+template <int place>
+__device__ __forceinline__ void load_to_lds(const void* base, uint32_t off, uint32_t lds) {
+  asm volatile("s_add_u32 m0, %0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3" ::"s"(lds), "n"(place), "v"(off),
+               "s"(base)
+               : "scc");
+}
+template <int place>
 __device__ __forceinline__ void load_to_lds(const void* src, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(src) : "memory");
+  asm volatile("s_add_u32 m0, %0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off" ::"s"(lds), "n"(place), "v"(src)
+               : "scc");
 }
-// Every load of this wave has arrived and its LDS accesses are done; then all waves meet.
-__device__ __forceinline__ void stage_barrier() {
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+// The same with 4 bytes per lane.
+__device__ __forceinline__ void word_to_lds(const void* src, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(src));
 }
 
-// XOR pattern of the 16-byte pieces of k-outer rows: four neighbouring k of a
-// transposed read (bf16), or the two k groups of the half waves (fp32), go to
-// different banks.
+// All but the last `newest` of this wave's loads and stores are done (they are
+// counted in order).
+template <int newest>
+__device__ __forceinline__ void wait_memory() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(newest) : "memory");
+}
+// The wave's LDS accesses are done; then all waves meet.
+__device__ __forceinline__ void wave_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// XOR pattern of a k-inner row's eight pieces: any eight or sixteen neighbouring
+// rows read at one piece touch different banks.
+__device__ __forceinline__ int inner_swizzle(int row) { return (row ^ (row >> 3 & 1)) & 7; }
+
+// XOR pattern of the 16-byte pieces of k-outer rows, the same for all rows of a
+// thread: four neighbouring k of a transposed read (bf16) go to different banks.
+// fp32 operands are read 4 bytes a lane, two lanes to a bank, which its matrix
+// instructions hide.
 template <typename T, int DIM>
 __device__ __forceinline__ int outer_swizzle(int k) {
-  constexpr int pieces = DIM * (int)sizeof(T) / 16;
-  if constexpr (sizeof(T) == 2)
-    return (4 * (k & 3)) & (pieces - 1);
-  else
-    return (8 * ((k >> 2) & 1)) & (pieces - 1);
+  return sizeof(T) == 2 ? (4 * (k & 3)) & (DIM * 2 / 16 - 1) : 0;
 }
 
-// Loads one operand's stages into LDS.  DIM operand rows (k inner) or columns
-// (k outer).  VEC: whole 16-byte pieces straight to LDS; else element by
-// element through registers, for rows of any width and alignment.
-template <typename T, int LAYOUT, int DIM, int THREADS, bool VEC>
-struct Loader {
+// A pointer that is the same in all lanes, in scalar registers.
+__device__ __forceinline__ const char* uniform(const char* p) {
+  const uint64_t v = reinterpret_cast<uint64_t>(p);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+  return reinterpret_cast<const char*>(((uint64_t)hi << 32) | lo);
+}
+
+// The lane, as a value that is only known here: what is computed from it is not
+// moved out of the loop to occupy registers throughout the kernel.
+__device__ __forceinline__ int here(int lane) {
+  asm volatile("" : "+v"(lane));
+  return lane;
+}
+
+// f(0), f(1), .. f(N - 1) with constant arguments.
+template <int N, typename F>
+__device__ __forceinline__ void each(F&& f) {
+  if constexpr (N > 0) {
+    each<N - 1>(f);
+    f(std::integral_constant<int, N - 1>{});
+  }
+}
+
+// Loads one operand's stages into LDS, whole 16-byte pieces straight from global
+// memory.  DIM operand rows (k inner) or columns (k outer).  A piece's address is
+// a uniform base, which moves with the stage, and an offset, which stays: 32 bits
+// of bytes, or of pieces where rows taken by token span 4 GiB or more (wide).
+// The last stage of a contraction may be short: the pieces past its end are
+// loaded from a place inside it, and once they have arrived their thread writes
+// zeros over them (clear).
+template <typename T, int LAYOUT, int DIM, int THREADS, bool WIDE, bool GATHER>
+struct PieceLoader {
   static constexpr int EL = Mma<T>::kElems;
-  static constexpr int KS = kStageBytes / (int)sizeof(T);           // k of a stage
-  static constexpr int N = DIM * kStageBytes / 16 / THREADS;        // pieces per thread
-  static constexpr int PR = LAYOUT == kInner ? 8 : DIM / EL;        // pieces of an LDS row
-  static constexpr int RS = THREADS / PR;                           // LDS rows between a thread's pieces
-  const T* ptr[N];
-  int32_t k;         // first k of the thread's next pieces (k inner: of the piece)
-  int32_t K;
-  int32_t left;      // k outer: elements of the row from the piece on
-  int64_t step;      // elements to the next stage
-  // gathered k-outer rows
+  static constexpr int KS = kStageBytes / (int)sizeof(T);     // k of a stage
+  static constexpr int N = DIM * kStageBytes / 16 / THREADS;  // pieces per thread
+  static constexpr int PR = LAYOUT == kInner ? kStageBytes / 16 : DIM / EL;  // pieces of an LDS row
+  static constexpr int RS = THREADS / PR;                     // LDS rows between a thread's pieces
+  static_assert(LAYOUT == kInner || (kWave % PR == 0 && (sizeof(T) == 4 || RS % 4 == 0)));
+  const char* base;      // of the stage
+  uint32_t off[N];
+  int64_t step;          // bytes to the next stage
+  int32_t left;          // k from the stage's first on
+  // gathered k-outer rows: their tokens come through LDS, kList of them at a time in two lists
+  uint32_t col, ldp;     // the thread's offset in a row, the length of a row
   const int32_t* token;
-  const T* base;
-  int64_t ld;
-  int64_t last;      // last row of the gathered operand
-  int32_t next[N];
+  uint32_t last;         // last row of the gathered operand
+  const int32_t* list;
+  uint32_t list_lds;     // its LDS byte address
+  int32_t pos, K;        // first k of the stage
+  int32_t turn = 0;      // the list in use
 
   static __device__ __forceinline__ int row(int tid) { return tid / PR; }
   static __device__ __forceinline__ int piece(int tid) {
     const int slot = tid % PR;
     if constexpr (LAYOUT == kInner)
-      return slot ^ (row(tid) & 7);
+      return slot ^ inner_swizzle(row(tid));
     else
       return slot ^ outer_swizzle<T, DIM>(row(tid));
   }
-
-  // k inner: rowp(i) is the start of operand row i of the tile
+  // the first k of a thread's piece in its stage
+  static __device__ __forceinline__ int first_k(int tid, int j) {
+    return LAYOUT == kInner ? piece(tid) * EL : row(tid) + j * RS;
+  }
+  // k inner: rowi(i, j) is the operand row of row i of the tile, the thread's j-th
   template <typename F>
-  __device__ __forceinline__ void start_inner(int tid, int32_t K_, F&& rowp) {
+  __device__ __forceinline__ void start_inner(int tid, int32_t K, const T* b, int32_t ld, F&& rowi) {
+    base = reinterpret_cast<const char*>(b);
+    left = K;
+    step = kStageBytes;
+    constexpr uint32_t unit = WIDE ? EL : 1, el = WIDE ? 1 : sizeof(T);
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      off[j] = (uint32_t)rowi(row(tid) + j * RS, j) * ((uint32_t)ld / unit * el) + piece(tid) * EL / unit * el;
+    shorten(tid);
+  }
+  // k outer: rows b + k * ld (or b + tok[k] * ld), columns col0 .. of `cols`
+  __device__ __forceinline__ void start_outer(int tid, int32_t K_, const T* b, int32_t ld, int32_t col0, int32_t cols,
+                                              const int32_t* tok_, int64_t last_, const int32_t* lists) {
+    base = reinterpret_cast<const char*>(b);
+    left = K = K_;
+    constexpr uint32_t unit = WIDE ? EL : 1, el = WIDE ? 1 : sizeof(T);
+    ldp = (uint32_t)ld / unit * el;
+    token = tok_;
+    last = (uint32_t)last_;
+    const int c = col0 + piece(tid) * EL;
+    col = (c < cols ? (uint32_t)c : 0u) / unit * el;  // a column tile's end: any place inside, the result is dropped
+    if constexpr (!GATHER) {
+      step = (int64_t)KS * ld * (int)sizeof(T);
+#pragma unroll
+      for (int j = 0; j < N; ++j) off[j] = (uint32_t)(row(tid) + j * RS) * ldp + col;
+      shorten(tid);
+    } else {
+      step = 0;
+      pos = 0;
+      list = lists;
+      list_lds = (uint32_t)(uintptr_t)(const DOL_LDS char*)(lists);
+      fetch(tid);
+    }
+  }
+  // A short stage: pieces past the end take the place of the first k.
+  __device__ __forceinline__ void shorten(int tid) {
+    if (left < KS) {
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const int kk = first_k(tid, j);
+        if (kk >= left)
+          off[j] -= LAYOUT == kInner ? (uint32_t)(WIDE ? kk / EL : kk * (int)sizeof(T)) : (uint32_t)kk * ldp;
+      }
+    }
+  }
+  // The tokens from k = pos on to the other list, which no wave reads since the last barrier: they
+  // have arrived at the next one.
+  __device__ __forceinline__ void fetch(int tid) {
+    turn ^= 1;
+    const uint32_t dst = list_lds + turn * kList * 4 + (uint32_t)(tid & ~63) * 4;
+#pragma unroll
+    for (int i = 0; i < kList / THREADS; ++i)
+      word_to_lds(token + max(0, min(pos + tid + i * THREADS, K - 1)),
+                  __builtin_amdgcn_readfirstlane(dst + i * THREADS * 4));
+  }
+  // Piece J of the stage to LDS byte address dst (uniform: the wave's place in the operand's stage).
+  template <int J>
+  __device__ __forceinline__ void load(int tid, uint32_t dst) {
+    uint32_t o = off[J];
+    if constexpr (GATHER)  // an index below 0 is clamped to the last row
+      o = min((uint32_t)list[turn * kList + (pos & (kList - 1)) + row(tid) + J * RS], last) * ldp + col;
+    if constexpr (WIDE)
+      load_to_lds<J * THREADS * 16>(base + (uint64_t)o * 16, dst);
+    else
+      load_to_lds<J * THREADS * 16>(uniform(base), o, dst);
+  }
+  __device__ __forceinline__ void next(int tid) {
+    if constexpr (GATHER) {
+      pos += KS;
+      if ((pos & (kList - 1)) == 0) fetch(tid);
+    }
+    base += step;
+    left -= KS;
+    if constexpr (!GATHER) shorten(tid);
+  }
+  // Zeros over the pieces past the end of a stage with `have` k, which has arrived.
+  static __device__ __forceinline__ void clear(int tid, int have, char* st) {
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if (first_k(tid, j) >= have) *reinterpret_cast<v4u*>(st + (tid + j * THREADS) * 16) = v4u{0u, 0u, 0u, 0u};
+  }
+};
+
+// The same for rows of any width and alignment, element by element through
+// registers.
+template <typename T, int LAYOUT, int DIM, int THREADS>
+struct ElementLoader {
+  static constexpr int EL = Mma<T>::kElems;
+  static constexpr int KS = kStageBytes / (int)sizeof(T);
+  static constexpr int N = DIM * kStageBytes / 16 / THREADS;
+  static constexpr int PR = LAYOUT == kInner ? kStageBytes / 16 : DIM / EL;
+  static constexpr int RS = THREADS / PR;
+  const T* ptr[N];
+  int32_t k;     // first k of the thread's next pieces (k inner: of the piece)
+  int32_t K;
+  int32_t cols;  // k outer: elements of the row from the piece on
+  int64_t ld;
+  const int32_t* token;
+  const T* base;
+  int64_t last;
+
+  static __device__ __forceinline__ int row(int tid) { return tid / PR; }
+  static __device__ __forceinline__ int piece(int tid) {
+    const int slot = tid % PR;
+    if constexpr (LAYOUT == kInner)
+      return slot ^ inner_swizzle(row(tid));
+    else
+      return slot ^ outer_swizzle<T, DIM>(row(tid));
+  }
+  template <typename F>
+  __device__ __forceinline__ void start_inner(int tid, int32_t K_, const T* b, int32_t ld_, F&& rowi) {
     K = K_;
     k = piece(tid) * EL;
-    step = KS;
 #pragma unroll
-    for (int j = 0; j < N; ++j) ptr[j] = rowp(row(tid) + j * RS) + k;
+    for (int j = 0; j < N; ++j) ptr[j] = b + (int64_t)rowi(row(tid) + j * RS, j) * ld_ + k;
   }
-  // k outer: rows base + k * ld (or base + token[k] * ld), columns col0 .. of `cols`
-  __device__ __forceinline__ void start_outer(int tid, int32_t K_, const T* base_, int64_t ld_, int32_t col0,
-                                              int32_t cols, const int32_t* token_, int64_t last_) {
+  __device__ __forceinline__ void start_outer(int tid, int32_t K_, const T* b, int32_t ld_, int32_t col0,
+                                              int32_t cols_, const int32_t* tok, int64_t last_, const int32_t*) {
     K = K_;
     k = row(tid);
     ld = ld_;
-    step = (int64_t)KS * ld;
-    token = token_;
+    token = tok;
     last = last_;
-    int c = col0 + piece(tid) * EL;
-    left = cols - c;
-    if (left <= 0) c = 0;  // a column tile's end: any valid address, the result is dropped
-    base = base_ + c;
-    if (token == nullptr) {
-#pragma unroll
-      for (int j = 0; j < N; ++j) ptr[j] = base + (int64_t)(k + j * RS) * ld;
-    } else {
-      fetch(0);
-    }
+    const int c = col0 + piece(tid) * EL;
+    cols = cols_ - c;
+    base = b + (cols > 0 ? c : 0);
   }
-  __device__ __forceinline__ void fetch(int ahead) {
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const int kk = k + j * RS + ahead;
-      next[j] = kk < K ? token[kk] : 0;
-    }
-  }
-
-  __device__ __forceinline__ const T* at(int j) const {
+  template <int J>
+  __device__ __forceinline__ void load(int tid, char* dst) {
+    const int kk = LAYOUT == kInner ? k : k + J * RS;
+    const int n = kk >= K ? 0 : (LAYOUT == kInner ? K - kk : cols);  // elements that exist
+    const T* src = ptr[J];
     if constexpr (LAYOUT == kOuter) {
-      if (token != nullptr) {
-        int64_t r = next[j];
-        r = r < 0 ? 0 : (r > last ? last : r);
-        return base + r * ld;
+      int64_t r = kk;
+      if (token != nullptr && kk < K) {
+        r = token[kk];
+        r = r < 0 || r > last ? last : r;
       }
+      src = base + r * ld;
     }
-    return ptr[j];
+    union {
+      T el[EL];
+      v4u v;
+    } u;
+    u.v = v4u{0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int i = 0; i < EL; ++i)
+      if (i < n) u.el[i] = src[i];
+    *reinterpret_cast<v4u*>(dst + (tid + J * THREADS) * 16) = u.v;
   }
-
-  // Loads the next stage to LDS byte address dst (its generic pointer: dstp).
-  __device__ __forceinline__ void stage(int tid, uint32_t dst, char* dstp) {
-    const uint32_t wave_dst = __builtin_amdgcn_readfirstlane(dst + (uint32_t)(tid & ~63) * 16);
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const int kk = LAYOUT == kInner ? k : k + j * RS;
-      const T* src = at(j);
-      if constexpr (VEC) {
-        const void* from = kk < K ? (const void*)src : (const void*)&zero_piece;
-        load_to_lds(from, wave_dst + j * THREADS * 16);
-      } else {
-        const int n = kk >= K ? 0 : (LAYOUT == kInner ? K - kk : left);  // elements that exist
-        union {
-          T el[EL];
-          v4u v;
-        } u;
-        u.v = v4u{0u, 0u, 0u, 0u};
-#pragma unroll
-        for (int i = 0; i < EL; ++i)
-          if (i < n) u.el[i] = src[i];
-        *reinterpret_cast<v4u*>(dstp + (tid + j * THREADS) * 16) = u.v;
-      }
-    }
-    if constexpr (LAYOUT == kOuter) {
-      if (token != nullptr) fetch(KS);
-    }
+  __device__ __forceinline__ void next(int) {
     k += KS;
+    if constexpr (LAYOUT == kInner) {
 #pragma unroll
-    for (int j = 0; j < N; ++j) ptr[j] += step;
+      for (int j = 0; j < N; ++j) ptr[j] += KS;
+    }
   }
 };
 
@@ -224,7 +366,7 @@ struct Reader {
   __device__ __forceinline__ void start(int lane, int base) {
     if constexpr (LAYOUT == kInner) {
       off = (base + (lane & 31)) * kStageBytes;
-      sw = (lane >> 5) ^ (lane & 7);
+      sw = (lane >> 5) ^ inner_swizzle(lane & 31);
       col = 0;
     } else if constexpr (sizeof(T) == 2) {
       const int k = 8 * (lane >> 5) + ((lane & 15) >> 2);
@@ -260,6 +402,11 @@ struct Reader {
   }
 };
 
+// Between LDS writes and reads of a staging area by other lanes of the wave (in
+// both orders): a wave's LDS accesses are executed in order, so only the
+// compiler has to keep them so.
+__device__ __forceinline__ void wave_fence() { asm volatile("" ::: "memory"); }
+
 __device__ __forceinline__ int32_t clip_rows(int32_t v, int64_t R) {
   return v < 0 ? 0 : ((int64_t)v > R ? (int32_t)R : v);
 }
@@ -276,6 +423,7 @@ __device__ __forceinline__ char* staged(char* area, int row, int byte) {
 template <typename T>
 __device__ __forceinline__ void store_rows(char* area, int lane, T* dst, int64_t ld, int rows, int cols, bool vec) {
   constexpr int EL = 16 / (int)sizeof(T);
+  wave_fence();
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int row = i * 8 + (lane >> 3), c = (lane & 7) * EL;
@@ -296,6 +444,7 @@ __device__ __forceinline__ void store_rows(char* area, int lane, T* dst, int64_t
       }
     }
   }
+  wave_fence();
 }
 
 // Writes a lane's 16 outputs of one 32 x 32 tile to its staged row: outputs
@@ -331,20 +480,24 @@ __device__ __forceinline__ void store_pair(char* area, int lane, const v16f& a0,
   }
 }
 
-// 32 rows of 64 fp32 outputs (two matrix tiles) in 8 KiB, the 16-byte pieces
-// XOR-ed with the row.
+// 16 of the 32 rows of 64 fp32 outputs (two matrix tiles) in 4 KiB, the 16-byte
+// pieces XOR-ed with the row.
 __device__ __forceinline__ char* staged_wide(char* area, int row, int piece) {
-  return area + row * 256 + ((piece ^ (row & 15)) << 4);
+  return area + row * 256 + ((piece ^ row) << 4);
 }
-__device__ __forceinline__ void stage_wide(char* area, int lane, const v16f& a0, const v16f& a1) {
-  const int row = lane & 31, h = lane >> 5;
+__device__ __forceinline__ void stage_wide(char* area, int lane, int half, const v16f& a0, const v16f& a1) {
+  const int row = lane & 15, h = lane >> 5;
+  wave_fence();
+  if (((lane >> 4) & 1) == half) {
 #pragma unroll
-  for (int b = 0; b < 4; ++b) {
-    *reinterpret_cast<v4f*>(staged_wide(area, row, 2 * b + h)) =
-        v4f{a0[4 * b], a0[4 * b + 1], a0[4 * b + 2], a0[4 * b + 3]};
-    *reinterpret_cast<v4f*>(staged_wide(area, row, 8 + 2 * b + h)) =
-        v4f{a1[4 * b], a1[4 * b + 1], a1[4 * b + 2], a1[4 * b + 3]};
+    for (int b = 0; b < 4; ++b) {
+      *reinterpret_cast<v4f*>(staged_wide(area, row, 2 * b + h)) =
+          v4f{a0[4 * b], a0[4 * b + 1], a0[4 * b + 2], a0[4 * b + 3]};
+      *reinterpret_cast<v4f*>(staged_wide(area, row, 8 + 2 * b + h)) =
+          v4f{a1[4 * b], a1[4 * b + 1], a1[4 * b + 2], a1[4 * b + 3]};
+    }
   }
+  wave_fence();
 }
 // Eight outputs from column c (a multiple of 8) of a staged row.
 __device__ __forceinline__ void read_wide(char* area, int row, int c, float* v) {
@@ -381,6 +534,28 @@ __device__ __forceinline__ void store_eight(T* d, const float* v, int n, bool ve
   }
 }
 
+// Stores the first n of four values to d, at once when vec (then n is 4).
+template <typename T>
+__device__ __forceinline__ void store_four(T* d, const v4f& v, int n, bool vec) {
+  if constexpr (sizeof(T) == 2) {
+    if (vec) {
+      *reinterpret_cast<v2u*>(d) = v2u{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < n) d[i] = bf16_bits(v[i]);
+  } else {
+    if (vec) {
+      *reinterpret_cast<v4f*>(d) = v;
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < n) d[i] = v[i];
+  }
+}
+
 __device__ __forceinline__ float sigmoid(float g) { return 1.0f / (1.0f + __expf(-g)); }
 
 __device__ __forceinline__ float prob_at(const ExpertGemm& g, int64_t i) {
@@ -395,12 +570,15 @@ __device__ __forceinline__ float row_prob(const ExpertGemm& g, int64_t r, int e)
   return prob_at(g, t * g.E + e);
 }
 
-template <typename T, typename C, int LP, int LQ, int EPI, bool VEC>
+template <typename T, typename C, int LP, int LQ, int EPI, int LOAD, bool GP, bool GQ>
 __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const ExpertGemm g) {
-  extern __shared__ __align__(16) char sm[];  // two stages, then the tile list
+  extern __shared__ __align__(16) char sm[];  // two stages, token lists, the tile list
   constexpr int KS = kStageBytes / (int)sizeof(T);
   constexpr int BPo = EPI == kSwiglu ? C::BP / 2 : C::BP;  // output columns of a tile
-  int32_t* first = reinterpret_cast<int32_t*>(sm + 2 * C::stage);  // [E + 1] first tile of each expert
+  int32_t* first = reinterpret_cast<int32_t*>(sm + 2 * C::stage);  // [E + 1] first tile of an expert
+  int32_t* lists = reinterpret_cast<int32_t*>(sm + 2 * C::stage);  // of tokens, two for each gathered operand
+  first += ((GP ? 2 : 0) + (GQ ? 2 : 0)) * kList;
+  int32_t* begin = first + g.E + 1;                                // [E + 1] first row of an expert
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int wp = wave % C::WP, wq = wave / C::WP;
   const int PT = (g.Pd + BPo - 1) / BPo;
@@ -412,12 +590,13 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
       const int e = e0 + lane;
       int n = 0;
       if (e < g.E) {
-        if constexpr (EPI == kWeightGrad) {
+        const int b = clip_rows(g.offsets[e], g.R), c = clip_rows(g.offsets[e + 1], g.R);
+        begin[e] = b;
+        if (e == g.E - 1) begin[g.E] = c;
+        if constexpr (EPI == kWeightGrad)
           n = PT * QT;
-        } else {
-          n = clip_rows(g.offsets[e + 1], g.R) - clip_rows(g.offsets[e], g.R);
-          n = n > 0 ? (n + C::BQ - 1) / C::BQ * PT : 0;
-        }
+        else
+          n = c > b ? (c - b + C::BQ - 1) / C::BQ * PT : 0;
       }
 #pragma unroll
       for (int d = 1; d < kWave; d <<= 1) {
@@ -430,23 +609,27 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
     if (lane == 0) first[0] = 0;
   }
   __syncthreads();
-  const int total = first[g.E];
+  const int total = __builtin_amdgcn_readfirstlane(first[g.E]);
   const int xcd = blockIdx.x & 7;
   int tile = (int)((int64_t)total * xcd >> 3) + (int)(blockIdx.x >> 3);
   const int tile_end = (int)((int64_t)total * (xcd + 1) >> 3);
   const int tile_step = (int)(gridDim.x >> 3);
   if (tile >= tile_end) return;
 
-  Loader<T, LP, C::BP, C::threads, VEC> lp;
-  Loader<T, LQ, C::BQ, C::threads, VEC> lq;
+  constexpr bool VEC = LOAD != kElements, WIDE = LOAD == kWidePieces;
+  using LoaderP = std::conditional_t<VEC, PieceLoader<T, LP, C::BP, C::loaders, WIDE, GP>, ElementLoader<T, LP, C::BP, C::loaders>>;
+  using LoaderQ = std::conditional_t<VEC, PieceLoader<T, LQ, C::BQ, C::loaders, WIDE, GQ>, ElementLoader<T, LQ, C::BQ, C::loaders>>;
+  LoaderP lp;
+  LoaderQ lq;
   Reader<T, LP, C::BP> rp;
   Reader<T, LQ, C::BQ> rq;
-  rp.start(lane, wp * 64);
+  rp.start(lane, wp * (C::BP / C::WP));
   rq.start(lane, wq * (C::BQ / C::WQ));
 
   // where a tile's outputs go
   struct Where {
-    int32_t e, p0, q0, r0, rows, nk;  // q0: weight gradients; r0, rows: the tile's rows
+    int32_t e, p0, q0, r0, rows;  // q0: weight gradients; r0, rows: the tile's rows
+    int32_t have, nk;             // contraction, its stages
   };
   auto locate = [&](int t) {
     Where w;
@@ -456,142 +639,228 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
     e = __builtin_amdgcn_readfirstlane(e);
     w.e = e;
     const int i = t - first[e];
-    const int b = clip_rows(g.offsets[e], g.R), n = max(0, clip_rows(g.offsets[e + 1], g.R) - b);
+    const int b = begin[e], n = max(0, begin[e + 1] - b);
     w.p0 = __builtin_amdgcn_readfirstlane((i % PT) * BPo);
     if constexpr (EPI == kWeightGrad) {
       w.q0 = __builtin_amdgcn_readfirstlane(i / PT * C::BQ);
       w.r0 = __builtin_amdgcn_readfirstlane(b);
       w.rows = __builtin_amdgcn_readfirstlane(n);
-      w.nk = max(1, (w.rows + KS - 1) / KS);
+      w.have = w.rows;
     } else {
       w.q0 = 0;
       w.r0 = __builtin_amdgcn_readfirstlane(b + i / PT * C::BQ);
       w.rows = __builtin_amdgcn_readfirstlane(min(C::BQ, n - i / PT * C::BQ));
-      w.nk = (g.K + KS - 1) / KS;
+      w.have = g.K;
     }
+    w.nk = max(1, (w.have + KS - 1) / KS);
     return w;
   };
-  auto start = [&](const Where& w) {
+  // the tokens of a thread's rows of a tile, loaded ahead of start()
+  struct Tokens {
+    int32_t t[LoaderQ::N];
+  };
+  auto tokens = [&](const Where& w) {
+    Tokens k;
+    if constexpr (EPI != kWeightGrad) {
+#pragma unroll
+      for (int j = 0; j < LoaderQ::N; ++j)
+        if (g.q_token != nullptr) k.t[j] = g.q_token[w.r0 + min(LoaderQ::row(tid) + j * LoaderQ::RS, w.rows - 1)];
+    }
+    return k;
+  };
+  auto start = [&](const Where& w, const Tokens& k) {
     const T* P = static_cast<const T*>(g.P);
     const T* Q = static_cast<const T*>(g.Q);
     if constexpr (EPI == kWeightGrad) {
-      const int32_t* pt = g.p_token ? g.p_token + w.r0 : nullptr;
-      const int32_t* qt = g.q_token ? g.q_token + w.r0 : nullptr;
-      lp.start_outer(tid, w.rows, pt ? P : P + (int64_t)w.r0 * g.ldp, g.ldp, w.p0, g.Pd, pt, g.N - 1);
-      lq.start_outer(tid, w.rows, qt ? Q : Q + (int64_t)w.r0 * g.ldq, g.ldq, w.q0, g.Qd, qt, g.N - 1);
+      // an expert without rows may begin at the lists' end, where there is no token to look at
+      const int32_t t0 = (int32_t)min((int64_t)w.r0, g.R - 1);
+      const int32_t* pt = g.p_token ? g.p_token + t0 : nullptr;
+      const int32_t* qt = g.q_token ? g.q_token + t0 : nullptr;
+      lp.start_outer(tid, w.rows, pt ? P : P + (int64_t)w.r0 * g.ldp, g.ldp, w.p0, g.Pd, pt, g.N - 1, lists);
+      lq.start_outer(tid, w.rows, qt ? Q : Q + (int64_t)w.r0 * g.ldq, g.ldq, w.q0, g.Qd, qt, g.N - 1, lists + (GP ? 2 * kList : 0));
     } else {
       if constexpr (LP == kInner) {
         // the gated activation takes 32 gate rows and the 32 up rows beside them for each wave
-        const T* we = P + (int64_t)w.e * (EPI == kSwiglu ? 2 * g.Pd : g.Pd) * g.ldp;
-        lp.start_inner(tid, g.K, [&](int i) {
-          int64_t row;
-          if constexpr (EPI == kSwiglu)
-            row = min(w.p0 + (i >> 6) * 32 + (i & 31), g.Pd - 1) + (int64_t)((i >> 5) & 1) * g.Pd;
-          else
-            row = min(w.p0 + i, g.Pd - 1);
-          return we + row * g.ldp;
-        });
+        lp.start_inner(tid, g.K, P + (int64_t)w.e * (EPI == kSwiglu ? 2 * g.Pd : g.Pd) * g.ldp, g.ldp,
+                       [&](int i, int) {
+                         if constexpr (EPI == kSwiglu)
+                           return min(w.p0 + (i >> 6) * 32 + (i & 31), g.Pd - 1) + ((i >> 5) & 1) * g.Pd;
+                         else
+                           return min(w.p0 + i, g.Pd - 1);
+                       });
       } else {
-        lp.start_outer(tid, g.K, P + (int64_t)w.e * g.K * g.ldp, g.ldp, w.p0, g.Pd, nullptr, 0);
+        lp.start_outer(tid, g.K, P + (int64_t)w.e * g.K * g.ldp, g.ldp, w.p0, g.Pd, nullptr, 0, nullptr);
       }
-      lq.start_inner(tid, g.K, [&](int i) {
-        int64_t row = w.r0 + min(i, w.rows - 1);
-        if (g.q_token != nullptr) {
-          row = g.q_token[row];
-          row = row < 0 ? 0 : (row >= g.N ? g.N - 1 : row);
-        }
-        return Q + row * g.ldq;
-      });
+      if (g.q_token != nullptr) {
+        const uint32_t last = (uint32_t)g.N - 1u;
+        lq.start_inner(tid, g.K, Q, g.ldq, [&](int, int j) { return min((uint32_t)k.t[j], last); });
+      } else {
+        lq.start_inner(tid, g.K, Q + (int64_t)w.r0 * g.ldq, g.ldq,
+                       [&](int i, int) { return min(i, w.rows - 1); });
+      }
     }
   };
-  const uint32_t sm_lds = (uint32_t)(uintptr_t)(DOL_LDS char*)sm;
-  auto load = [&](int buf) {
-    lp.stage(tid, sm_lds + buf * C::stage, sm + buf * C::stage);
-    lq.stage(tid, sm_lds + buf * C::stage + C::BP * kStageBytes, sm + buf * C::stage + C::BP * kStageBytes);
+  const uint32_t wave_lds = (uint32_t)(uintptr_t)(DOL_LDS char*)sm + (uint32_t)(tid & ~63) * 16;
+
+  // The loaders run a stage ahead of the products, through the tiles in the same order.
+  const bool loader = wave < C::waves / 2;
+  Where wl = locate(tile);
+  int load_tile = tile, load_left = wl.nk, load_slot = 0;
+  int32_t load_have = wl.have, have = wl.have;  // k from the next stage's first on, and from the last loaded one's
+  bool loading = true;
+  Tokens kn;
+  if (loader) {
+    start(wl, tokens(wl));
+    if (load_tile + tile_step < tile_end) {
+      wl = locate(load_tile + tile_step);
+      kn = tokens(wl);
+    }
+  }
+  // piece I of a thread's pieces of the next stage, P's then Q's
+  constexpr int kLoads = LoaderP::N + LoaderQ::N;
+  auto load = [&](auto which) {
+    constexpr int I = decltype(which)::value;
+    const int at = load_slot * C::stage + (I < LoaderP::N ? 0 : C::BP * kStageBytes);
+    auto one = [&](auto& l, auto piece) {
+      if constexpr (VEC)
+        l.template load<decltype(piece)::value>(tid, __builtin_amdgcn_readfirstlane(wave_lds + at));
+      else
+        l.template load<decltype(piece)::value>(tid, sm + at);
+    };
+    if constexpr (I < LoaderP::N)
+      one(lp, std::integral_constant<int, I>{});
+    else
+      one(lq, std::integral_constant<int, I - LoaderP::N>{});
+  };
+  auto load_stage = [&] {
+    if (!loading) return;
+    each<kLoads>([&](auto i) { load(i); });
+    load_slot ^= 1;
+    have = load_have;
+    if (--load_left > 0) {
+      lp.next(tid);
+      lq.next(tid);
+      load_have -= KS;
+    } else {
+      load_tile += tile_step;
+      loading = load_tile < tile_end;
+      if (loading) {
+        start(wl, kn);
+        load_left = wl.nk;
+        load_have = wl.have;
+        if (load_tile + tile_step < tile_end) {
+          wl = locate(load_tile + tile_step);
+          kn = tokens(wl);
+        }
+      }
+    }
+  };
+  // Once the loads of the stage in a buffer have arrived: zeros past the end of a short one.
+  auto clear = [&](int b) {
+    if constexpr (VEC) {
+      if (have < KS) {
+        LoaderP::clear(tid, have, sm + b * C::stage);
+        LoaderQ::clear(tid, have, sm + b * C::stage + C::BP * kStageBytes);
+      }
+    }
   };
 
-  Where w = locate(tile);
-  start(w);
+  using Frag = typename Mma<T>::Frag;
+  struct Frags {
+    Frag p[C::MP], q[C::MQ];
+  };
+  // the operands of phase s of the stage in a buffer
+  auto read = [&](Frags& f, int buf, int s) {
+    const char* sp = sm + buf * C::stage;
+    const char* sq = sp + C::BP * kStageBytes;
+#pragma unroll
+    for (int i = 0; i < C::MP; ++i) f.p[i] = rp.get(sp, i, s);
+#pragma unroll
+    for (int j = 0; j < C::MQ; ++j) f.q[j] = rq.get(sq, j, s);
+  };
+
+  if constexpr (GP || GQ) {  // the first lists
+    wait_memory<0>();
+    wave_barrier();
+  }
+  if (loader) {
+    load_stage();
+    __builtin_amdgcn_s_setprio(1);  // it begins to multiply later than the other wave of its SIMD
+  }
   int buf = 0;
-  load(0);
-  for (;;) {
+  for (; tile < tile_end; tile += tile_step) {
+    const Where w = locate(tile);
     v16f acc[C::MP][C::MQ];
 #pragma unroll
     for (int i = 0; i < C::MP; ++i)
 #pragma unroll
       for (int j = 0; j < C::MQ; ++j) acc[i][j] = v16f{};
-    tile += tile_step;
-    const bool more = tile < tile_end;
-    Where wn = w;
+    auto multiply = [&](const Frags& f) {
+#pragma unroll
+      for (int j = 0; j < C::MQ; ++j)
+#pragma unroll
+        for (int i = 0; i < C::MP; ++i) acc[i][j] = Mma<T>::mul(f.p[i], f.q[j], acc[i][j]);
+    };
     for (int ks = 0; ks < w.nk; ++ks) {
-      stage_barrier();
-      if (ks + 1 < w.nk) {
-        load(buf ^ 1);
-      } else if (more) {
-        wn = locate(tile);
-        start(wn);
-        load(buf ^ 1);
+      if (loader) {
+        wait_memory<0>();
+        clear(buf);
       }
-      const char* sp = sm + buf * C::stage;
-      const char* sq = sp + C::BP * kStageBytes;
-#pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        typename Mma<T>::Frag fp[C::MP], fq[C::MQ];
-#pragma unroll
-        for (int i = 0; i < C::MP; ++i) fp[i] = rp.get(sp, i, s);
-#pragma unroll
-        for (int j = 0; j < C::MQ; ++j) fq[j] = rq.get(sq, j, s);
-#pragma unroll
-        for (int i = 0; i < C::MP; ++i)
-#pragma unroll
-          for (int j = 0; j < C::MQ; ++j) acc[i][j] = Mma<T>::mul(fp[i], fq[j], acc[i][j]);
+      wave_barrier();
+      if (loader) load_stage();
+      #pragma unroll
+      for (int s = 0; s < kPhases; ++s) {
+        Frags f;
+        read(f, buf, s);
+        multiply(f);
       }
       buf ^= 1;
     }
-    // The stage just used (buf ^ 1) holds the staging areas: every wave is done with it, and the
-    // next tile's second stage is loaded into it only after the barrier of its first.
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    // The stage just used holds the waves' areas once every wave is done with it; it is loaded again
+    // only after the next barrier.
+    wave_barrier();
     char* area = sm + (buf ^ 1) * C::stage + wave * (C::stage / C::waves);
-    const int qw = wq * (C::BQ / C::WQ);
+    const int qw = wq * (C::BQ / C::WQ), pw = wp * (C::BP / C::WP);
     if constexpr (EPI == kStore) {
       T* y = static_cast<T*>(g.out);
 #pragma unroll
-      for (int j = 0; j < C::MQ; ++j) {
-        const int c = w.p0 + wp * 64, r = qw + j * 32;
-        store_pair<T>(area, lane, acc[0][j], acc[1][j], y + (int64_t)(w.r0 + r) * g.Pd + c, g.Pd, w.rows - r,
+      for (int ij = 0; ij < C::MP / 2 * C::MQ; ++ij) {
+        const int i = ij / C::MQ * 2, j = ij % C::MQ, c = w.p0 + pw + 32 * i, r = qw + j * 32;
+        store_pair<T>(area, lane, acc[i][j], acc[i + 1][j], y + (int64_t)(w.r0 + r) * g.Pd + c, g.Pd, w.rows - r,
                       g.Pd - c, g.vec_out);
       }
     } else if constexpr (EPI == kWeightGrad) {
       float* dw = static_cast<float*>(g.out) + (int64_t)w.e * g.Qd * g.Pd;
 #pragma unroll
-      for (int j = 0; j < C::MQ; ++j) {
-        const int c = w.p0 + wp * 64, r = w.q0 + qw + j * 32;
+      for (int ij = 0; ij < C::MP / 2 * C::MQ; ++ij) {
+        const int i = ij / C::MQ * 2, j = ij % C::MQ, c = w.p0 + pw + 32 * i, r = w.q0 + qw + j * 32;
         float* d = dw + (int64_t)r * g.Pd + c;
         if (g.accumulate) {
           const int row = r + (lane & 31), c0 = c + 4 * (lane >> 5);
           if (row < g.Qd) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int ii = 0; ii < 2; ++ii)
 #pragma unroll
               for (int v = 0; v < 16; ++v) {
-                const int cc = 32 * i + 8 * (v >> 2) + (v & 3);
-                if (c0 + cc < g.Pd) acc[i][j][v] += dw[(int64_t)row * g.Pd + c0 + cc];
+                const int cc = 32 * ii + 8 * (v >> 2) + (v & 3);
+                if (c0 + cc < g.Pd) acc[i + ii][j][v] += dw[(int64_t)row * g.Pd + c0 + cc];
               }
           }
         }
-        store_pair<float>(area, lane, acc[0][j], acc[1][j], d, g.Pd, g.Qd - r, g.Pd - c, g.vec_out);
+        store_pair<float>(area, lane, acc[i][j], acc[i + 1][j], d, g.Pd, g.Qd - r, g.Pd - c, g.vec_out);
       }
     } else if constexpr (EPI == kSwiglu) {
       // 32 rows at a time: gate and up of 32 activations in fp32 to the staging area, then four
       // lanes take a row, eight activations each (a lane's group of 32 is its four lanes')
       const int F = g.Pd, G = (F + kAct8Group - 1) / kAct8Group;
-      const int f0 = w.p0 + wp * 32, c = (lane & 3) * 8, n = min(8, F - f0 - c);
 #pragma unroll
-      for (int j = 0; j < C::MQ; ++j) {
-        stage_wide(area, lane, acc[0][j], acc[1][j]);
+      for (int ij = 0; ij < C::MP / 2 * C::MQ; ++ij) {
+        const int j = ij % C::MQ, f0 = w.p0 + pw / 2 + ij / C::MQ * 32;
 #pragma unroll 1
         for (int i = 0; i < 2; ++i) {
-          const int row = i * 16 + (lane >> 2), rr = qw + j * 32 + row;
+          stage_wide(area, lane, i, acc[ij / C::MQ * 2][j], acc[ij / C::MQ * 2 + 1][j]);
+          const int ln = here(lane), c = (ln & 3) * 8, n = min(8, F - f0 - c);
+          const int row = ln >> 2, rr = qw + j * 32 + i * 16 + row;
           float a[2][8];
           read_wide(area, row, c, a[0]);
           read_wide(area, row, 32 + c, a[1]);
@@ -632,43 +901,41 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
         }
       }
     } else {
-      // dh = W2^T dy of 64 activations and 32 rows at a time in fp32 to the staging area; then
-      // eight lanes take a row, eight activations each, with gate and up from their 8-bit values
+      // dh = W2^T dy of 64 activations and 16 rows at a time in fp32 to the staging area; then
+      // 16 lanes take a row, four activations each, with gate and up from their 8-bit values
       const int F = g.Pd, G = (F + kAct8Group - 1) / kAct8Group;
-      const int f0 = w.p0 + wp * 64, c = (lane & 7) * 8, n = min(8, F - f0 - c);
 #pragma unroll
-      for (int j = 0; j < C::MQ; ++j) {
-        stage_wide(area, lane, acc[0][j], acc[1][j]);
+      for (int ij = 0; ij < C::MP / 2 * C::MQ; ++ij) {
+        const int j = ij % C::MQ, f0 = w.p0 + pw + ij / C::MQ * 64;
 #pragma unroll 1
-        for (int i = 0; i < 4; ++i) {
-          const int row = i * 8 + (lane >> 3), rr = qw + j * 32 + row;
-          const bool live = rr < w.rows && n > 0;
+        for (int i = 0; i < 8; ++i) {
+          if (i % 4 == 0) stage_wide(area, lane, i / 4, acc[ij / C::MQ * 2][j], acc[ij / C::MQ * 2 + 1][j]);
+          const int ln = here(lane), c = (ln & 15) * 4, n = min(4, F - f0 - c);
+          const int row = (i & 3) * 4 + (ln >> 4), rr = qw + j * 32 + i / 4 * 16 + row;
           const int64_t r = w.r0 + rr;
-          float dh[8];
-          read_wide(area, row, c, dh);
+          const v4f dh = *reinterpret_cast<const v4f*>(staged_wide(area, row, c >> 2));
           float dp = 0.0f;
-          if (live) {
-            v2u qg = v2u{0u, 0u}, qu = v2u{0u, 0u};
+          if (rr < w.rows && n > 0) {
+            uint32_t qg = 0, qu = 0;
             const int8_t* q = g.q8 + r * 2 * F + f0 + c;
             if (g.vec_q8) {
-              qg = *reinterpret_cast<const v2u*>(q);
-              qu = *reinterpret_cast<const v2u*>(q + F);
+              qg = *reinterpret_cast<const uint32_t*>(q);
+              qu = *reinterpret_cast<const uint32_t*>(q + F);
             } else {
 #pragma unroll
-              for (int v = 0; v < 8; ++v)
+              for (int v = 0; v < 4; ++v)
                 if (v < n) {
-                  qg[v >> 2] |= (uint32_t)(uint8_t)q[v] << (8 * (v & 3));
-                  qu[v >> 2] |= (uint32_t)(uint8_t)q[F + v] << (8 * (v & 3));
+                  qg |= (uint32_t)(uint8_t)q[v] << (8 * v);
+                  qu |= (uint32_t)(uint8_t)q[F + v] << (8 * v);
                 }
             }
             const uint8_t* eb = g.e8 + r * 2 * G + (f0 + c) / kAct8Group;
             const float sg = act8_scale(eb[0]), su = act8_scale(eb[G]);
             const float p = row_prob(g, r, w.e);
-            float dg[8], du[8], hv[8];
+            v4f dg, du, hv;
 #pragma unroll
-            for (int v = 0; v < 8; ++v) {
-              const float gt = (float)(int8_t)(qg[v >> 2] >> (8 * (v & 3))) * sg;
-              const float up = (float)(int8_t)(qu[v >> 2] >> (8 * (v & 3))) * su;
+            for (int v = 0; v < 4; ++v) {
+              const float gt = (float)(int8_t)(qg >> (8 * v)) * sg, up = (float)(int8_t)(qu >> (8 * v)) * su;
               const float z = sigmoid(gt), sl = gt * z, ds = p * dh[v];
               dp += v < n ? dh[v] * (sl * up) : 0.0f;
               hv[v] = p * (sl * up);
@@ -676,28 +943,27 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
               dg[v] = ds * up * (z * (1.0f + gt * (1.0f - z)));
             }
             T* da = static_cast<T*>(g.out) + r * 2 * F + f0 + c;
-            store_eight<T>(da, dg, n, g.vec_out);
-            store_eight<T>(da + F, du, n, g.vec_out);
-            store_eight<T>(static_cast<T*>(g.out2) + r * F + f0 + c, hv, n, g.vec_out);
+            store_four<T>(da, dg, n, g.vec_out);
+            store_four<T>(da + F, du, n, g.vec_out);
+            store_four<T>(static_cast<T*>(g.out2) + r * F + f0 + c, hv, n, g.vec_out);
           }
           if (g.dp != nullptr && f0 < F) {
             dp += __shfl_xor(dp, 1);
             dp += __shfl_xor(dp, 2);
             dp += __shfl_xor(dp, 4);
-            if ((lane & 7) == 0 && rr < w.rows) g.dp[(int64_t)(f0 / 64) * g.R + r] = dp;
+            dp += __shfl_xor(dp, 8);
+            if ((ln & 15) == 0 && rr < w.rows) g.dp[(int64_t)(f0 / 64) * g.R + r] = dp;
           }
         }
       }
     }
-    if (!more) break;
-    w = wn;
   }
 }
 
-template <typename T, typename C, int LP, int LQ, int EPI, bool VEC>
+template <typename T, typename C, int LP, int LQ, int EPI, int LOAD, bool GP = false, bool GQ = false>
 hipError_t launch_gemm(const ExpertGemm& g, hipStream_t s) {
-  const void* kern = reinterpret_cast<const void*>(k_expert_gemm<T, C, LP, LQ, EPI, VEC>);
-  const size_t lds = 2 * (size_t)C::stage + (size_t)(g.E + 1) * 4;
+  const void* kern = reinterpret_cast<const void*>(k_expert_gemm<T, C, LP, LQ, EPI, LOAD, GP, GQ>);
+  const size_t lds = 2 * (size_t)C::stage + ((GP ? 2 : 0) + (GQ ? 2 : 0)) * kList * 4 + (size_t)(g.E + 1) * 8;
   hipError_t e = hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
   if (e != hipSuccess) return e;
   int occ = 0;
@@ -710,15 +976,20 @@ hipError_t launch_gemm(const ExpertGemm& g, hipStream_t s) {
                                            : PT * (g.R / C::BQ + std::min<int64_t>(g.E, g.R));
   if (tiles >= (int64_t(1) << 31)) return hipErrorInvalidValue;
   const int64_t blocks = std::min<int64_t>((tiles + 7) & ~int64_t(7), (int64_t)occ * device_info().cu_count & ~int64_t(7));
-  hipLaunchKernelGGL((k_expert_gemm<T, C, LP, LQ, EPI, VEC>), dim3((unsigned)std::max<int64_t>(8, blocks)),
+  hipLaunchKernelGGL((k_expert_gemm<T, C, LP, LQ, EPI, LOAD, GP, GQ>), dim3((unsigned)std::max<int64_t>(8, blocks)),
                      dim3(C::threads), lds, s, g);
   return hipGetLastError();
 }
 
-template <typename T, int LP, int LQ, int EPI>
+// big: the large tile.  Operands that are not whole pieces go element by element; rows by token
+// that span 4 GiB or more take wide offsets, on the small tile.
+// GP, GQ: k-outer rows of P and Q are taken by token (an element loader looks at the list itself).
+template <typename T, int LP, int LQ, int EPI, bool GP = false, bool GQ = false>
 hipError_t pick_gemm(const ExpertGemm& g, bool big, bool vec, hipStream_t s) {
-  if (big) return vec ? launch_gemm<T, Big, LP, LQ, EPI, true>(g, s) : launch_gemm<T, Big, LP, LQ, EPI, false>(g, s);
-  return vec ? launch_gemm<T, Small, LP, LQ, EPI, true>(g, s) : launch_gemm<T, Small, LP, LQ, EPI, false>(g, s);
+  if (!vec)
+    return big ? launch_gemm<T, Big, LP, LQ, EPI, kElements>(g, s) : launch_gemm<T, Small, LP, LQ, EPI, kElements>(g, s);
+  if (g.wide) return launch_gemm<T, Small, LP, LQ, EPI, kWidePieces, GP, GQ>(g, s);
+  return big ? launch_gemm<T, Big, LP, LQ, EPI, kPieces, GP, GQ>(g, s) : launch_gemm<T, Small, LP, LQ, EPI, kPieces, GP, GQ>(g, s);
 }
 
 }  // namespace expert

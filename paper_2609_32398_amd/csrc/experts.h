@@ -40,6 +40,7 @@ struct ExpertGemm {
   int32_t Qd;              // weight gradients: extent of q (rows of an expert's gradient)
   int32_t K;               // contraction (weight gradients: the rows of an expert)
   int32_t ldp, ldq;        // elements of a row of P and Q
+  int32_t wide;            // rows taken by token span 4 GiB or more
   int32_t accumulate;      // weight gradients: add to what is there
   int32_t vec_out;         // rows of the outputs take 16-byte stores
   int32_t vec_q8;          // rows of the 8-bit values take 8-byte accesses
@@ -53,7 +54,8 @@ struct ExpertGemm {
 };
 
 hipError_t launch_expert_matmul(const ExpertGemm& g, do_dtype dt, bool transposed, bool vec, hipStream_t s);
-hipError_t launch_expert_weight_grad(const ExpertGemm& g, do_dtype dt, bool vec, hipStream_t s);
+hipError_t launch_expert_weight_grad_bf16(const ExpertGemm& g, bool big, bool vec, hipStream_t s);
+hipError_t launch_expert_weight_grad_f32(const ExpertGemm& g, bool big, bool vec, hipStream_t s);
 hipError_t launch_expert_swiglu(const ExpertGemm& g, do_dtype dt, bool vec, hipStream_t s);
 hipError_t launch_expert_swiglu_grad(const ExpertGemm& g, do_dtype dt, bool vec, hipStream_t s);
 // dp [N][E] (fp32 or bf16) from the partial sums: zero where a token has no row.
