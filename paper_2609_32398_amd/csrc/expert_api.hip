@@ -273,7 +273,7 @@ DOLOSS_API do_status do_expert_swiglu_grad(const void* dy, const void* w2, do_dt
   g.out2 = h;
   g.dp = dp != nullptr ? static_cast<float*>(workspace) : nullptr;
   g.vec_out = aligned(da, 16) && aligned(h, 16) && F % 8 == 0;
-  g.vec_q8 = aligned(q, 8) && F % 8 == 0;
+  g.vec_q8 = aligned(q, 16) && F % 16 == 0;
   DO_TRY(launched(dol::launch_expert_swiglu_grad(g, dtype, whole(dy, dtype, H, N) && whole(w2, dtype, F), stream)));
   if (dp == nullptr) return DO_OK;
   return launched(dol::launch_expert_dp(g.dp, (F + 63) / 64, R, token_row, token_expert, N, k, E, dp, p_dtype, stream));

@@ -570,14 +570,19 @@ __device__ __forceinline__ float row_prob(const ExpertGemm& g, int64_t r, int e)
   return prob_at(g, t * g.E + e);
 }
 
+template <typename C, int EPI>
+constexpr int kProbs = EPI == kSwiglu || EPI == kSwigluGrad ? C::BQ : 0;
+
 template <typename T, typename C, int LP, int LQ, int EPI, int LOAD, bool GP, bool GQ>
 __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const ExpertGemm g) {
-  extern __shared__ __align__(16) char sm[];  // two stages, token lists, the tile list
+  extern __shared__ __align__(16) char sm[];  // two stages, token lists, row probabilities, the tile list
   constexpr int KS = kStageBytes / (int)sizeof(T);
   constexpr int BPo = EPI == kSwiglu ? C::BP / 2 : C::BP;  // output columns of a tile
   int32_t* first = reinterpret_cast<int32_t*>(sm + 2 * C::stage);  // [E + 1] first tile of an expert
   int32_t* lists = reinterpret_cast<int32_t*>(sm + 2 * C::stage);  // of tokens, two for each gathered operand
   first += ((GP ? 2 : 0) + (GQ ? 2 : 0)) * kList;
+  float* probs = reinterpret_cast<float*>(first);  // of a tile's rows
+  first += kProbs<C, EPI>;
   int32_t* begin = first + g.E + 1;                                // [E + 1] first row of an expert
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int wp = wave % C::WP, wq = wave / C::WP;
@@ -801,6 +806,13 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
 #pragma unroll
         for (int i = 0; i < C::MP; ++i) acc[i][j] = Mma<T>::mul(f.p[i], f.q[j], acc[i][j]);
     };
+    // A tile's row probabilities: loaded now by the waves that load nothing else (a wait for them would
+    // include all loads before), used after the last stage.
+    float prob = 0.0f;
+    const int prob_row = tid - (C::threads - C::loaders);
+    static_assert(kProbs<C, EPI> <= C::threads - C::loaders);
+    if (kProbs<C, EPI> > 0 && prob_row >= 0 && prob_row < w.rows && prob_row < C::BQ)
+      prob = row_prob(g, w.r0 + prob_row, w.e);
     for (int ks = 0; ks < w.nk; ++ks) {
       if (loader) {
         wait_memory<0>();
@@ -816,6 +828,7 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
       }
       buf ^= 1;
     }
+    if (kProbs<C, EPI> > 0 && prob_row >= 0 && prob_row < C::BQ) probs[prob_row] = prob;
     // The stage just used holds the waves' areas once every wave is done with it; it is loaded again
     // only after the next barrier.
     wave_barrier();
@@ -866,7 +879,7 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
           read_wide(area, row, 32 + c, a[1]);
           const bool live = rr < w.rows;
           const int64_t r = w.r0 + rr;
-          const float p = live ? row_prob(g, r, w.e) : 0.0f;
+          const float p = probs[rr];
           float hv[8];
 #pragma unroll
           for (int v = 0; v < 8; ++v) hv[v] = p * (a[0][v] * sigmoid(a[0][v])) * a[1][v];
@@ -901,37 +914,64 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
         }
       }
     } else {
-      // dh = W2^T dy of 64 activations and 16 rows at a time in fp32 to the staging area; then
-      // 16 lanes take a row, four activations each, with gate and up from their 8-bit values
-      const int F = g.Pd, G = (F + kAct8Group - 1) / kAct8Group;
-#pragma unroll
-      for (int ij = 0; ij < C::MP / 2 * C::MQ; ++ij) {
-        const int j = ij % C::MQ, f0 = w.p0 + pw + ij / C::MQ * 64;
-#pragma unroll 1
-        for (int i = 0; i < 8; ++i) {
-          if (i % 4 == 0) stage_wide(area, lane, i / 4, acc[ij / C::MQ * 2][j], acc[ij / C::MQ * 2 + 1][j]);
-          const int ln = here(lane), c = (ln & 15) * 4, n = min(4, F - f0 - c);
-          const int row = (i & 3) * 4 + (ln >> 4), rr = qw + j * 32 + i / 4 * 16 + row;
-          const int64_t r = w.r0 + rr;
-          const v4f dh = *reinterpret_cast<const v4f*>(staged_wide(area, row, c >> 2));
-          float dp = 0.0f;
-          if (rr < w.rows && n > 0) {
-            uint32_t qg = 0, qu = 0;
-            const int8_t* q = g.q8 + r * 2 * F + f0 + c;
-            if (g.vec_q8) {
-              qg = *reinterpret_cast<const uint32_t*>(q);
-              qu = *reinterpret_cast<const uint32_t*>(q + F);
-            } else {
-#pragma unroll
-              for (int v = 0; v < 4; ++v)
-                if (v < n) {
-                  qg |= (uint32_t)(uint8_t)q[v] << (8 * v);
-                  qu |= (uint32_t)(uint8_t)q[F + v] << (8 * v);
-                }
+      // dh = W2^T dy of 64 activations and 16 rows at a time in fp32 to the staging area, with their
+      // 8-bit gate and up behind (128 bytes a row, loaded 16 rows ahead); then 16 lanes take a row,
+      // four activations each
+      const int F = g.Pd, G = (F + kAct8Group - 1) / kAct8Group, parts = (F + 63) / 64;
+      const int f0 = w.p0 + pw;
+      static_assert(C::MP == 2 && C::stage / C::waves >= 4096 + 2048);
+      struct Kept {
+        v4u gate, up;
+        uint32_t e;  // of row lane / 4: half lane / 2 % 2, group lane % 2
+      };
+      auto kept = [&](int block) {
+        const int ln = here(lane), rr = qw + block * 16 + (ln >> 2), c = f0 + (ln & 3) * 16;
+        const int64_t r = w.r0 + rr;
+        Kept k{v4u{0u, 0u, 0u, 0u}, v4u{0u, 0u, 0u, 0u}, 0u};
+        if (rr < w.rows) {
+          const int8_t* q = g.q8 + r * 2 * F + c;
+          if (g.vec_q8) {
+            if (c < F) {
+              k.gate = *reinterpret_cast<const v4u*>(q);
+              k.up = *reinterpret_cast<const v4u*>(q + F);
             }
-            const uint8_t* eb = g.e8 + r * 2 * G + (f0 + c) / kAct8Group;
-            const float sg = act8_scale(eb[0]), su = act8_scale(eb[G]);
-            const float p = row_prob(g, r, w.e);
+          } else {
+#pragma unroll
+            for (int v = 0; v < 16; ++v)
+              if (c + v < F) {
+                k.gate[v >> 2] |= (uint32_t)(uint8_t)q[v] << (8 * (v & 3));
+                k.up[v >> 2] |= (uint32_t)(uint8_t)q[F + v] << (8 * (v & 3));
+              }
+          }
+          const int grp = f0 / kAct8Group + (ln & 1);
+          if (grp < G) k.e = g.e8[(r * 2 + ((ln >> 1) & 1)) * G + grp];
+        }
+        return k;
+      };
+      char* qarea = area + 4096;
+      Kept next = kept(0);
+#pragma unroll
+      for (int j = 0; j < C::MQ; ++j) {
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const Kept k = next;
+          if (j * 2 + half + 1 < C::MQ * 2) next = kept(j * 2 + half + 1);
+          stage_wide(area, lane, half, acc[0][j], acc[1][j]);
+          *reinterpret_cast<v4u*>(staged(qarea, lane >> 2, (lane & 3) * 16)) = k.gate;
+          *reinterpret_cast<v4u*>(staged(qarea, lane >> 2, 64 + (lane & 3) * 16)) = k.up;
+          wave_fence();
+#pragma unroll 1
+          for (int i = 0; i < 4; ++i) {
+            const int ln = here(lane), c = (ln & 15) * 4, n = min(4, F - f0 - c);
+            const int row = i * 4 + (ln >> 4), rr = qw + j * 32 + half * 16 + row;
+            const int64_t r = w.r0 + rr;
+            const v4f dh = *reinterpret_cast<const v4f*>(staged_wide(area, row, c >> 2));
+            const uint32_t qg = *reinterpret_cast<const uint32_t*>(staged(qarea, row, c));
+            const uint32_t qu = *reinterpret_cast<const uint32_t*>(staged(qarea, row, 64 + c));
+            const float sg = act8_scale((uint32_t)__shfl((int)k.e, row * 4 + (c >> 5)));
+            const float su = act8_scale((uint32_t)__shfl((int)k.e, row * 4 + 2 + (c >> 5)));
+            const float p = probs[rr];
+            float dp = 0.0f;
             v4f dg, du, hv;
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
@@ -942,18 +982,21 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
               du[v] = ds * sl;
               dg[v] = ds * up * (z * (1.0f + gt * (1.0f - z)));
             }
-            T* da = static_cast<T*>(g.out) + r * 2 * F + f0 + c;
-            store_four<T>(da, dg, n, g.vec_out);
-            store_four<T>(da + F, du, n, g.vec_out);
-            store_four<T>(static_cast<T*>(g.out2) + r * F + f0 + c, hv, n, g.vec_out);
+            if (rr < w.rows && n > 0) {
+              T* da = static_cast<T*>(g.out) + r * 2 * F + f0 + c;
+              store_four<T>(da, dg, n, g.vec_out);
+              store_four<T>(da + F, du, n, g.vec_out);
+              store_four<T>(static_cast<T*>(g.out2) + r * F + f0 + c, hv, n, g.vec_out);
+            }
+            if (g.dp != nullptr && f0 < F) {
+              dp += __shfl_xor(dp, 1);
+              dp += __shfl_xor(dp, 2);
+              dp += __shfl_xor(dp, 4);
+              dp += __shfl_xor(dp, 8);
+              if ((ln & 15) == 0 && rr < w.rows) g.dp[r * parts + f0 / 64] = dp;
+            }
           }
-          if (g.dp != nullptr && f0 < F) {
-            dp += __shfl_xor(dp, 1);
-            dp += __shfl_xor(dp, 2);
-            dp += __shfl_xor(dp, 4);
-            dp += __shfl_xor(dp, 8);
-            if ((ln & 15) == 0 && rr < w.rows) g.dp[(int64_t)(f0 / 64) * g.R + r] = dp;
-          }
+          wave_fence();
         }
       }
     }
@@ -963,7 +1006,7 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
 template <typename T, typename C, int LP, int LQ, int EPI, int LOAD, bool GP = false, bool GQ = false>
 hipError_t launch_gemm(const ExpertGemm& g, hipStream_t s) {
   const void* kern = reinterpret_cast<const void*>(k_expert_gemm<T, C, LP, LQ, EPI, LOAD, GP, GQ>);
-  const size_t lds = 2 * (size_t)C::stage + ((GP ? 2 : 0) + (GQ ? 2 : 0)) * kList * 4 + (size_t)(g.E + 1) * 8;
+  const size_t lds = 2 * (size_t)C::stage + (((GP ? 2 : 0) + (GQ ? 2 : 0)) * kList + kProbs<C, EPI>) * 4 + (size_t)(g.E + 1) * 8;
   hipError_t e = hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
   if (e != hipSuccess) return e;
   int occ = 0;

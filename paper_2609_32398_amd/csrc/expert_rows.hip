@@ -8,7 +8,8 @@
 // tokens, so one block takes whole units and one wave takes one 64-token word
 // position of a unit: lane l is token 64 w + l, the word of an expert is the
 // wave's mask of the tokens that chose it, and the place of a token among them
-// is a population count below its lane.
+// is a population count below its lane.  A bit transpose gives each lane its
+// token's experts, of which it then visits only those that are set.
 //
 // Bound by latency and launches up to some thousand tokens; beyond, by the
 // scattered 4-byte stores of the three lists (12 N k bytes).
@@ -20,34 +21,48 @@ namespace dol {
 namespace {
 
 constexpr int kRowThreads = 512;  // eight waves: the eight words of a unit
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 
-__device__ __forceinline__ u64 lane_word(u64 v, int i) {
-  const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, i);
-  const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), i);
-  return ((u64)hi << 32) | lo;
+// 64 x 64 bit transpose across the lanes of a wave: bit t of lane e's word becomes
+// bit e of lane t's.  Six exchanges of blocks of 32, 16, .. 1 bits between the
+// lanes that differ in that bit.
+__device__ __forceinline__ u64 transpose_bits(u64 v) {
+  const int lane = threadIdx.x & 63;
+  constexpr u64 low[6] = {0x5555555555555555ull, 0x3333333333333333ull, 0x0F0F0F0F0F0F0F0Full,
+                          0x00FF00FF00FF00FFull, 0x0000FFFF0000FFFFull, 0x00000000FFFFFFFFull};
+#pragma unroll
+  for (int b = 5; b >= 0; --b) {
+    const int d = 1 << b;
+    const u64 o = ((u64)(uint32_t)__shfl_xor((int)(uint32_t)(v >> 32), d) << 32) |
+                  (uint32_t)__shfl_xor((int)(uint32_t)v, d);
+    v = (lane & d) ? (v & ~low[b]) | ((o & ~low[b]) >> d) : (v & low[b]) | ((o & low[b]) << d);
+  }
+  return v;
 }
 
-// The masks of unit u: mask[e * 8 + w] = tokens of word w that chose e.  A
-// token's choices past the k-th in expert order (never for Top-k signatures)
+// The masks of unit u: mask[e * 8 + w] = tokens of word w that chose e; and
+// chosen(i, v): v = the experts 64 i .. 64 i + 63 that the lane's token chose.
+// A token's choices past the k-th in expert order (never for Top-k signatures)
 // and bits at or past N are left out, so no list can overflow.
-__device__ __forceinline__ void unit_masks(const u64* bits, int64_t u, int64_t N, int32_t E, int32_t k, u64* mask) {
+template <typename F>
+__device__ __forceinline__ void unit_masks(const u64* bits, int64_t u, int64_t N, int32_t E, int32_t k, u64* mask,
+                                           F&& chosen) {
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int64_t t0 = u * 512 + w * 64;
   const u64 live = t0 >= N ? 0 : (N - t0 >= 64 ? ~u64(0) : (u64(1) << (N - t0)) - 1);
-  int have = 0;
+  int left = k;
   for (int e0 = 0; e0 < E; e0 += kWave) {
     const int e = e0 + lane;
     u64 mine = e < E && live != 0 ? bits[((u * E + e) << 3) + w] & live : 0;
-    const int n = min(kWave, E - e0);
-    for (int i = 0; i < n; ++i) {
-      const u64 m = lane_word(mine, i);
-      if (m == 0) continue;
-      const bool take = ((m >> lane) & 1) != 0 && have < k;
-      const u64 got = __ballot(take);
-      have += take;
-      if (got != m && lane == i) mine = got;
+    u64 ex = transpose_bits(mine);
+    const int n = __popcll(ex);
+    if (__ballot(n > left) != 0) {  // some token has too many: keep its first ones
+      for (int i = n; i > left; --i) ex &= ~(u64(1) << (63 - __clzll((long long)ex)));
+      mine = transpose_bits(ex);
     }
+    left -= __popcll(ex);
     if (e < E) mask[e * 8 + w] = mine;
+    chosen(e0, ex);
   }
 }
 
@@ -59,7 +74,7 @@ __global__ __launch_bounds__(kRowThreads) void k_row_counts(const u64* bits, int
   const int64_t u0 = (int64_t)blockIdx.x * U / gridDim.x, u1 = (int64_t)(blockIdx.x + 1) * U / gridDim.x;
   uint32_t c[kMaxE / kRowThreads] = {};
   for (int64_t u = u0; u < u1; ++u) {
-    unit_masks(bits, u, N, E, k, sm);
+    unit_masks(bits, u, N, E, k, sm, [](int, u64) {});
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kMaxE / kRowThreads; ++i) {
@@ -87,7 +102,12 @@ __global__ __launch_bounds__(kRowThreads) void k_rows(const u64* bits, int64_t N
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int64_t U = (N + 511) >> 9;
   const int64_t u0 = (int64_t)blockIdx.x * U / gridDim.x, u1 = (int64_t)(blockIdx.x + 1) * U / gridDim.x;
-  unit_masks(bits, u0, N, E, k, sm);
+  u64 ex[kMaxE / kWave];  // the experts of the lane's token
+  auto keep = [&](int e0, u64 v) {
+#pragma unroll
+    for (int i = 0; i < kMaxE / kWave; ++i) ex[i] = e0 == i * kWave ? v : ex[i];
+  };
+  unit_masks(bits, u0, N, E, k, sm, keep);
   __syncthreads();
   // loads of thread t's experts t, t + 512, and the rows that earlier chunks take of them
   uint32_t load[kMaxE / kRowThreads] = {}, before[kMaxE / kRowThreads] = {};
@@ -136,30 +156,23 @@ __global__ __launch_bounds__(kRowThreads) void k_rows(const u64* bits, int64_t N
   }
   for (int64_t u = u0; u < u1; ++u) {
     if (u != u0) {
-      unit_masks(bits, u, N, E, k, sm);
+      unit_masks(bits, u, N, E, k, sm, keep);
       __syncthreads();
     }
     const int64_t t = u * 512 + w * 64 + lane;
     int have = 0;
-    for (int e0 = 0; e0 < E; e0 += kWave) {
-      const int e = e0 + lane;
-      u64 mine = 0;
-      uint32_t at = 0;
-      if (e < E) {
-        mine = sm[e * 8 + w];
-        at = next[e];
-        for (int v = 0; v < 8; ++v) at += v < w ? (uint32_t)__popcll(sm[e * 8 + v]) : 0u;
-      }
-      const int n = min(kWave, E - e0);
-      for (int i = 0; i < n; ++i) {
-        const u64 m = lane_word(mine, i);
-        if (m == 0) continue;
-        const uint32_t first = (uint32_t)__builtin_amdgcn_readlane((int)at, i);
-        if ((m >> lane) & 1) {
-          const uint32_t r = first + __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0u));
+#pragma unroll
+    for (int i = 0; i < kMaxE / kWave; ++i) {
+      if (i * kWave < E) {
+        u64 v = ex[i];
+        while (v != 0) {
+          const int e = i * kWave + __ffsll((long long)v) - 1;
+          v &= v - 1;
+          uint32_t r = next[e] + (uint32_t)__popcll(sm[e * 8 + w] & ((u64(1) << lane) - 1));
+          for (int x = 0; x < w; ++x) r += (uint32_t)__popcll(sm[e * 8 + x]);
           row_token[r] = (int32_t)t;
           token_row[t * k + have] = (int32_t)r;
-          token_expert[t * k + have] = e0 + i;
+          token_expert[t * k + have] = e;
           ++have;
         }
       }
@@ -212,29 +225,72 @@ __global__ __launch_bounds__(256) void k_combine(const T* o, const int32_t* toke
   }
 }
 
-// dp[t][e] of the token's rows: the partial sums in order; zero elsewhere.
+// The same for rows of whole 16-byte pieces: one piece per thread, the k rows'
+// pieces in flight together.  Bound by memory: 65,536 tokens of 8 rows of 2,048
+// bf16 move 2.42 GB.
 template <typename T>
-__global__ __launch_bounds__(256) void k_expert_dp(const float* part, int32_t nparts, int64_t R,
-                                                   const int32_t* token_row, const int32_t* token_expert, int64_t N,
-                                                   int32_t k, int32_t E, T* dp) {
-  const int lane = threadIdx.x & 63;
-  for (int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); t < N; t += (int64_t)gridDim.x * 4) {
-    // lane j holds the token's j-th row and expert, 64 at a time; the wave then
-    // writes the row of dp, each lane looking its columns up among them
-    for (int e0 = 0; e0 < E; e0 += kWave) {
-      const int e = e0 + lane;
-      float v = 0.0f;
-      for (int j = 0; j < k; ++j) {
-        const int64_t r = token_row[t * k + j];
-        const int te = token_expert[t * k + j];
-        if (te == e && r >= 0 && r < R) {
-          v = 0.0f;
-          for (int i = 0; i < nparts; ++i) v += part[(int64_t)i * R + r];
-        }
+__global__ __launch_bounds__(256) void k_combine_pieces(const v4u* o, const int32_t* token_row, int64_t N, int32_t k,
+                                                        int64_t R, int32_t pieces, v4u* y) {
+  constexpr int EL = 16 / (int)sizeof(T);
+  const int64_t total = N * pieces;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    const int64_t t = total <= 0xFFFFFFFFll ? (uint32_t)i / (uint32_t)pieces : i / pieces;
+    const int64_t c = i - t * pieces;
+    float s[EL];
+#pragma unroll
+    for (int v = 0; v < EL; ++v) s[v] = 0.0f;
+    for (int j0 = 0; j0 < k; j0 += 8) {
+      v4u x[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int64_t r = j0 + j < k ? token_row[t * k + j0 + j] : -1;
+        x[j] = r >= 0 && r < R ? __builtin_nontemporal_load(o + r * pieces + c) : v4u{0u, 0u, 0u, 0u};
       }
-      if (e < E) dp[t * E + e] = from_float<T>(v);
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int v = 0; v < EL; ++v) {
+          if constexpr (sizeof(T) == 4)
+            s[v] += __uint_as_float(x[j][v]);
+          else
+            s[v] += bf16_float((uint16_t)(x[j][v >> 1] >> (16 * (v & 1))));
+        }
+    }
+    v4u out;
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int v = 0; v < 4; ++v) out[v] = __float_as_uint(s[v]);
+    } else {
+#pragma unroll
+      for (int v = 0; v < 4; ++v) out[v] = bf16_pair(s[2 * v], s[2 * v + 1]);
+    }
+    __builtin_nontemporal_store(out, y + i);
+  }
+}
+
+// dp[t][e] of the token's rows: the partial sums in order; zero elsewhere.
+// A block takes T tokens: their rows of dp in LDS, zeroed, a thread for each of
+// the tokens' experts, and the rows written as they lie in memory.
+template <typename T>
+__global__ __launch_bounds__(256) void k_expert_dp(const float* part, int32_t parts, int64_t R,
+                                                   const int32_t* token_row, const int32_t* token_expert, int64_t N,
+                                                   int32_t k, int32_t E, int32_t tokens, T* dp) {
+  extern __shared__ float rows[];  // [tokens][E]
+  const int64_t t0 = (int64_t)blockIdx.x * tokens;
+  const int n = (int)min((int64_t)tokens, N - t0);
+  for (int i = threadIdx.x; i < n * E; i += 256) rows[i] = 0.0f;
+  __syncthreads();
+  for (int i = threadIdx.x; i < n * k; i += 256) {
+    const int64_t r = token_row[t0 * k + i];
+    const int e = token_expert[t0 * k + i];
+    if (r >= 0 && r < R && e >= 0 && e < E) {
+      float v = 0.0f;
+      for (int p = 0; p < parts; ++p) v += part[r * parts + p];
+      rows[i / k * E + e] = v;
     }
   }
+  __syncthreads();
+  for (int i = threadIdx.x; i < n * E; i += 256) dp[t0 * E + i] = from_float<T>(rows[i]);
 }
 
 }  // namespace
@@ -262,6 +318,18 @@ hipError_t launch_expert_rows(const u64* bits, int64_t N, int32_t E, int32_t k, 
 
 hipError_t launch_expert_combine(const void* o, do_dtype dt, const int32_t* token_row, int64_t N, int32_t k, int64_t R,
                                  int32_t H, void* y, hipStream_t s) {
+  const int el = dt == DO_F32 ? 4 : 8;
+  if (H % el == 0 && ((reinterpret_cast<uintptr_t>(o) | reinterpret_cast<uintptr_t>(y)) & 15) == 0) {
+    const int32_t pieces = H / el;
+    const dim3 grid((unsigned)std::min<int64_t>((N * pieces + 255) / 256, 1 << 20));
+    if (dt == DO_F32)
+      hipLaunchKernelGGL(k_combine_pieces<float>, grid, dim3(256), 0, s, static_cast<const v4u*>(o), token_row, N, k,
+                         R, pieces, static_cast<v4u*>(y));
+    else
+      hipLaunchKernelGGL(k_combine_pieces<uint16_t>, grid, dim3(256), 0, s, static_cast<const v4u*>(o), token_row, N,
+                         k, R, pieces, static_cast<v4u*>(y));
+    return hipGetLastError();
+  }
   const dim3 grid((unsigned)std::min<int64_t>(N, 65536), (unsigned)((H + 255) / 256));
   if (dt == DO_F32)
     hipLaunchKernelGGL(k_combine<float>, grid, dim3(256), 0, s, static_cast<const float*>(o), token_row, N, k, R, H,
@@ -275,13 +343,15 @@ hipError_t launch_expert_combine(const void* o, do_dtype dt, const int32_t* toke
 hipError_t launch_expert_dp(const float* part, int32_t nparts, int64_t R, const int32_t* token_row,
                             const int32_t* token_expert, int64_t N, int32_t k, int32_t E, void* dp, do_dtype dt,
                             hipStream_t s) {
-  const dim3 grid((unsigned)std::min<int64_t>((N + 3) / 4, 65536));
+  const int tokens = std::max(1, std::min(256 / k, 8192 / E));  // about one expert a thread, 32 KiB at most
+  const dim3 grid((unsigned)((N + tokens - 1) / tokens));
+  const size_t lds = (size_t)tokens * E * sizeof(float);
   if (dt == DO_F32)
-    hipLaunchKernelGGL(k_expert_dp<float>, grid, dim3(256), 0, s, part, nparts, R, token_row, token_expert, N, k, E,
-                       static_cast<float*>(dp));
+    hipLaunchKernelGGL(k_expert_dp<float>, grid, dim3(256), lds, s, part, nparts, R, token_row, token_expert, N, k, E,
+                       tokens, static_cast<float*>(dp));
   else
-    hipLaunchKernelGGL(k_expert_dp<uint16_t>, grid, dim3(256), 0, s, part, nparts, R, token_row, token_expert, N, k,
-                       E, static_cast<uint16_t*>(dp));
+    hipLaunchKernelGGL(k_expert_dp<uint16_t>, grid, dim3(256), lds, s, part, nparts, R, token_row, token_expert, N, k,
+                       E, tokens, static_cast<uint16_t*>(dp));
   return hipGetLastError();
 }
 

@@ -43,14 +43,14 @@ struct ExpertGemm {
   int32_t wide;            // rows taken by token span 4 GiB or more
   int32_t accumulate;      // weight gradients: add to what is there
   int32_t vec_out;         // rows of the outputs take 16-byte stores
-  int32_t vec_q8;          // rows of the 8-bit values take 8-byte accesses
+  int32_t vec_q8;          // rows of the 8-bit values take 8-byte stores (forward) or 16-byte loads
   int32_t p_bf16;          // type of prob
   const void* prob;        // nullable [N][E] routing probabilities
   int8_t* q8;              // [R][2][F] 8-bit gate and up values (written, or read by the backward pass)
   uint8_t* e8;             // [R][2][G] their exponents
   void* out;
   void* out2;              // backward pass: the activations again
-  float* dp;               // backward pass: partial sums of the probabilities' gradient, [ceil(F / 64)][R]
+  float* dp;               // backward pass: partial sums of the probabilities' gradient, [R][ceil(F / 64)]
 };
 
 hipError_t launch_expert_matmul(const ExpertGemm& g, do_dtype dt, bool transposed, bool vec, hipStream_t s);
