@@ -37,7 +37,8 @@ __global__ __launch_bounds__(256) void k_act8_pack(const T* x, int64_t rows, int
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, d));
     const uint32_t byte = act8_exponent(m);
-    if (c < W) q[row * W + c] = (int8_t)act8_round(v, act8_inverse(byte), byte);
+    const float one[4] = {v, 0.0f, 0.0f, 0.0f};
+    if (c < W) q[row * W + c] = (int8_t)act8_round4(one, act8_inverse(byte), byte);
     if (lane == 0) e[g] = (uint8_t)byte;
   }
 }
@@ -88,9 +89,7 @@ __global__ __launch_bounds__(256) void k_act8_pack_pieces(const T* x, int64_t gr
     m = max(m, (uint32_t)__shfl_xor((int)m, 2));
     const uint32_t byte = act8_exponent(m);
     const float inv = act8_inverse(byte);
-    v2u out = v2u{0u, 0u};
-#pragma unroll
-    for (int c = 0; c < 8; ++c) out[c >> 2] |= ((uint32_t)act8_round(v[c], inv, byte) & 255u) << (8 * (c & 3));
+    const v2u out = v2u{act8_round4(v, inv, byte), act8_round4(v + 4, inv, byte)};
     __builtin_nontemporal_store(out, reinterpret_cast<v2u*>(q) + i);
     if ((i & 3) == 0) e[i >> 2] = (uint8_t)byte;
   }
@@ -103,8 +102,8 @@ __global__ __launch_bounds__(256) void k_act8_unpack_pieces(const int8_t* q, con
     const v2u a = __builtin_nontemporal_load(reinterpret_cast<const v2u*>(q) + i);
     const float s = act8_scale(e[i >> 2]);
     float v[8];
-#pragma unroll
-    for (int c = 0; c < 8; ++c) v[c] = (float)(int8_t)(a[c >> 2] >> (8 * (c & 3))) * s;
+    act8_values4(a[0], s, v);
+    act8_values4(a[1], s, v + 4);
     if constexpr (sizeof(T) == 4) {
       v4u b, c;
 #pragma unroll

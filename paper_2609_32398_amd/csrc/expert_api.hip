@@ -132,8 +132,8 @@ DOLOSS_API do_status do_expert_matmul(const void* x, const void* w, do_dtype dty
   g.out = y;
   g.wide = row_token != nullptr && wide(dtype, in, N);
   g.vec_out = whole(y, dtype, out);
-  return launched(
-      dol::launch_expert_matmul(g, dtype, transposed != 0, whole(w, dtype, I) && whole(x, dtype, in, row_token != nullptr ? N : R), stream));
+  return launched((dtype == DO_F32 ? dol::launch_expert_matmul_f32 : dol::launch_expert_matmul_bf16)(
+      g, transposed != 0, whole(w, dtype, I) && whole(x, dtype, in, row_token != nullptr ? N : R), stream));
 }
 
 DOLOSS_API do_status do_expert_weight_grad(const void* dy, const void* x, do_dtype dtype, const int32_t* offsets,

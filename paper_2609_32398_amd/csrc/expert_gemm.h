@@ -154,11 +154,13 @@ __device__ __forceinline__ void each(F&& f) {
 
 // Loads one operand's stages into LDS, whole 16-byte pieces straight from global
 // memory.  DIM operand rows (k inner) or columns (k outer).  A piece's address is
-// a uniform base, which moves with the stage, and an offset, which stays: 32 bits
-// of bytes, or of pieces where rows taken by token span 4 GiB or more (wide).
-// The last stage of a contraction may be short: the pieces past its end are
-// loaded from a place inside it, and once they have arrived their thread writes
-// zeros over them (clear).
+// a uniform base, which moves with the stage, and an offset: 32 bits of bytes, or
+// of pieces where rows taken by token span 4 GiB or more (WIDE).  A thread's
+// pieces lie a uniform distance apart, so that one offset does for all (and a
+// limit, where a tile ends short); only rows taken by token (GATHER) have an
+// offset each.  The last stage of a contraction may be short: the pieces past its
+// end are loaded from a place inside it, and once they have arrived their thread
+// writes zeros over them (clear).
 template <typename T, int LAYOUT, int DIM, int THREADS, bool WIDE, bool GATHER>
 struct PieceLoader {
   static constexpr int EL = Mma<T>::kElems;
@@ -166,19 +168,22 @@ struct PieceLoader {
   static constexpr int N = DIM * kStageBytes / 16 / THREADS;  // pieces per thread
   static constexpr int PR = LAYOUT == kInner ? kStageBytes / 16 : DIM / EL;  // pieces of an LDS row
   static constexpr int RS = THREADS / PR;                     // LDS rows between a thread's pieces
+  static constexpr uint32_t kUnit = WIDE ? EL : 1, kBytes = WIDE ? 1 : sizeof(T);  // elements / kUnit * kBytes: offsets
   static_assert(LAYOUT == kInner || (kWave % PR == 0 && (sizeof(T) == 4 || RS % 4 == 0)));
-  const char* base;      // of the stage
-  uint32_t off[N];
-  int64_t step;          // bytes to the next stage
-  int32_t left;          // k from the stage's first on
-  // gathered k-outer rows: their tokens come through LDS, kList of them at a time in two lists
-  uint32_t col, ldp;     // the thread's offset in a row, the length of a row
+  const char* base;  // of the stage
+  int64_t step;      // bytes to the next stage
+  int32_t left;      // k from the stage's first on
+  uint32_t ldo;      // offset from row to row
+  // k inner, by token: the pieces' offsets.  Else the first one's, and the largest (k inner) or that of
+  // its column in the stage's first row (k outer).
+  uint32_t off[LAYOUT == kInner && GATHER ? N : 1], lim;
+  // k outer, by token: the tokens come through LDS, kList of them at a time in two lists
   const int32_t* token;
-  uint32_t last;         // last row of the gathered operand
+  uint32_t last;       // last row of the gathered operand
   const int32_t* list;
-  uint32_t list_lds;     // its LDS byte address
-  int32_t pos, K;        // first k of the stage
-  int32_t turn = 0;      // the list in use
+  uint32_t list_lds;   // its LDS byte address
+  int32_t pos, K;      // first k of the stage
+  int32_t turn = 0;    // the list in use
 
   static __device__ __forceinline__ int row(int tid) { return tid / PR; }
   static __device__ __forceinline__ int piece(int tid) {
@@ -192,50 +197,55 @@ struct PieceLoader {
   static __device__ __forceinline__ int first_k(int tid, int j) {
     return LAYOUT == kInner ? piece(tid) * EL : row(tid) + j * RS;
   }
-  // k inner: rowi(i, j) is the operand row of row i of the tile, the thread's j-th
+  // k inner, rows by token: rowi(j) is the operand row of the thread's j-th piece
   template <typename F>
-  __device__ __forceinline__ void start_inner(int tid, int32_t K, const T* b, int32_t ld, F&& rowi) {
-    base = reinterpret_cast<const char*>(b);
-    left = K;
+  __device__ __forceinline__ void start_rows(int tid, int32_t K_, const T* b, int32_t ld, F&& rowi) {
+    begin(K_, b, ld);
     step = kStageBytes;
-    constexpr uint32_t unit = WIDE ? EL : 1, el = WIDE ? 1 : sizeof(T);
 #pragma unroll
-    for (int j = 0; j < N; ++j)
-      off[j] = (uint32_t)rowi(row(tid) + j * RS, j) * ((uint32_t)ld / unit * el) + piece(tid) * EL / unit * el;
+    for (int j = 0; j < N; ++j) off[j] = (uint32_t)rowi(j) * ldo + piece(tid) * EL / kUnit * kBytes;
+    shorten(tid);
+  }
+  // k inner: rows b + (row0 + i) * ld, not past row `end`
+  __device__ __forceinline__ void start_inner(int tid, int32_t K_, const T* b, int32_t ld, int32_t row0, int32_t end) {
+    begin(K_, b, ld);
+    step = kStageBytes;
+    off[0] = (uint32_t)(row0 + row(tid)) * ldo + piece(tid) * EL / kUnit * kBytes;
+    lim = (uint32_t)end * ldo + piece(tid) * EL / kUnit * kBytes;
     shorten(tid);
   }
   // k outer: rows b + k * ld (or b + tok[k] * ld), columns col0 .. of `cols`
   __device__ __forceinline__ void start_outer(int tid, int32_t K_, const T* b, int32_t ld, int32_t col0, int32_t cols,
-                                              const int32_t* tok_, int64_t last_, const int32_t* lists) {
-    base = reinterpret_cast<const char*>(b);
-    left = K = K_;
-    constexpr uint32_t unit = WIDE ? EL : 1, el = WIDE ? 1 : sizeof(T);
-    ldp = (uint32_t)ld / unit * el;
-    token = tok_;
-    last = (uint32_t)last_;
+                                              const int32_t* tok, int64_t last_, const int32_t* lists) {
+    begin(K_, b, ld);
     const int c = col0 + piece(tid) * EL;
-    col = (c < cols ? (uint32_t)c : 0u) / unit * el;  // a column tile's end: any place inside, the result is dropped
-    if constexpr (!GATHER) {
-      step = (int64_t)KS * ld * (int)sizeof(T);
-#pragma unroll
-      for (int j = 0; j < N; ++j) off[j] = (uint32_t)(row(tid) + j * RS) * ldp + col;
-      shorten(tid);
-    } else {
+    lim = (c < cols ? (uint32_t)c : 0u) / kUnit * kBytes;  // a column tile's end: any place inside, the result is dropped
+    if constexpr (GATHER) {
       step = 0;
+      token = tok;
+      last = (uint32_t)last_;
       pos = 0;
       list = lists;
       list_lds = (uint32_t)(uintptr_t)(const DOL_LDS char*)(lists);
       fetch(tid);
+    } else {
+      step = (int64_t)KS * ld * (int)sizeof(T);
+      off[0] = (uint32_t)row(tid) * ldo + lim;
     }
   }
-  // A short stage: pieces past the end take the place of the first k.
+  __device__ __forceinline__ void begin(int32_t K_, const T* b, int32_t ld) {
+    base = reinterpret_cast<const char*>(b);
+    left = K = K_;
+    ldo = (uint32_t)ld / kUnit * kBytes;
+  }
+  // A short stage, k inner: pieces past the end take the place of the first k.
   __device__ __forceinline__ void shorten(int tid) {
-    if (left < KS) {
+    if constexpr (LAYOUT == kInner) {
+      if (left < KS && first_k(tid, 0) >= left) {
+        const uint32_t back = (uint32_t)first_k(tid, 0) / kUnit * kBytes;
+        lim -= back;
 #pragma unroll
-      for (int j = 0; j < N; ++j) {
-        const int kk = first_k(tid, j);
-        if (kk >= left)
-          off[j] -= LAYOUT == kInner ? (uint32_t)(WIDE ? kk / EL : kk * (int)sizeof(T)) : (uint32_t)kk * ldp;
+        for (int j = 0; j < (GATHER ? N : 1); ++j) off[j] -= back;
       }
     }
   }
@@ -250,24 +260,35 @@ struct PieceLoader {
                   __builtin_amdgcn_readfirstlane(dst + i * THREADS * 4));
   }
   // Piece J of the stage to LDS byte address dst (uniform: the wave's place in the operand's stage).
+  // far: where the rows of piece J lie from those of piece 0 (k inner).
   template <int J>
-  __device__ __forceinline__ void load(int tid, uint32_t dst) {
-    uint32_t o = off[J];
-    if constexpr (GATHER)  // an index below 0 is clamped to the last row
-      o = min((uint32_t)list[turn * kList + (pos & (kList - 1)) + row(tid) + J * RS], last) * ldp + col;
+  __device__ __forceinline__ void load(int tid, uint32_t dst, uint32_t far, uint32_t up) {
+    uint32_t o;
+    if constexpr (LAYOUT == kOuter) {
+      if constexpr (GATHER) {  // an index below 0 is clamped to the last row
+        o = min((uint32_t)list[turn * kList + (pos & (kList - 1)) + row(tid) + J * RS], last) * ldo + lim;
+      } else {
+        o = off[0] + J * RS * ldo;
+        if (left < KS) o = first_k(tid, J) < left ? o : lim;
+      }
+    } else if constexpr (GATHER) {
+      o = off[J];
+    } else {
+      o = min(off[0] + far * ldo, lim) + up;
+    }
     if constexpr (WIDE)
       load_to_lds<J * THREADS * 16>(base + (uint64_t)o * 16, dst);
     else
       load_to_lds<J * THREADS * 16>(uniform(base), o, dst);
   }
   __device__ __forceinline__ void next(int tid) {
-    if constexpr (GATHER) {
+    if constexpr (LAYOUT == kOuter && GATHER) {
       pos += KS;
       if ((pos & (kList - 1)) == 0) fetch(tid);
     }
     base += step;
     left -= KS;
-    if constexpr (!GATHER) shorten(tid);
+    shorten(tid);
   }
   // Zeros over the pieces past the end of a stage with `have` k, which has arrived.
   static __device__ __forceinline__ void clear(int tid, int have, char* st) {
@@ -304,11 +325,11 @@ struct ElementLoader {
       return slot ^ outer_swizzle<T, DIM>(row(tid));
   }
   template <typename F>
-  __device__ __forceinline__ void start_inner(int tid, int32_t K_, const T* b, int32_t ld_, F&& rowi) {
+  __device__ __forceinline__ void start_rows(int tid, int32_t K_, const T* b, int32_t ld_, F&& rowi) {
     K = K_;
     k = piece(tid) * EL;
 #pragma unroll
-    for (int j = 0; j < N; ++j) ptr[j] = b + (int64_t)rowi(row(tid) + j * RS, j) * ld_ + k;
+    for (int j = 0; j < N; ++j) ptr[j] = b + (int64_t)rowi(j) * ld_ + k;
   }
   __device__ __forceinline__ void start_outer(int tid, int32_t K_, const T* b, int32_t ld_, int32_t col0,
                                               int32_t cols_, const int32_t* tok, int64_t last_, const int32_t*) {
@@ -556,7 +577,8 @@ __device__ __forceinline__ void store_four(T* d, const v4f& v, int n, bool vec) 
   }
 }
 
-__device__ __forceinline__ float sigmoid(float g) { return 1.0f / (1.0f + __expf(-g)); }
+// 1 / (1 + e^-g), the quotient by the hardware's reciprocal (one unit in the last place off at most).
+__device__ __forceinline__ float sigmoid(float g) { return __builtin_amdgcn_rcpf(1.0f + __expf(-g)); }
 
 __device__ __forceinline__ float prob_at(const ExpertGemm& g, int64_t i) {
   return g.p_bf16 ? bf16_float(static_cast<const uint16_t*>(g.prob)[i]) : static_cast<const float*>(g.prob)[i];
@@ -565,11 +587,14 @@ __device__ __forceinline__ float prob_at(const ExpertGemm& g, int64_t i) {
 // The routing probability of row r of expert e (1 without probabilities).
 __device__ __forceinline__ float row_prob(const ExpertGemm& g, int64_t r, int e) {
   if (g.prob == nullptr) return 1.0f;
-  int64_t t = g.q_token != nullptr ? g.q_token[r] : r;
+  int64_t t = g.q_token[r];
   t = t < 0 ? 0 : (t >= g.N ? g.N - 1 : t);
   return prob_at(g, t * g.E + e);
 }
 
+// LDS beside the stages: lists of tokens (k outer only) and probabilities of a tile's rows.
+template <int EPI, bool GP, bool GQ>
+constexpr int kLists = EPI == kWeightGrad ? (GP ? 2 : 0) + (GQ ? 2 : 0) : 0;
 template <typename C, int EPI>
 constexpr int kProbs = EPI == kSwiglu || EPI == kSwigluGrad ? C::BQ : 0;
 
@@ -580,7 +605,7 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
   constexpr int BPo = EPI == kSwiglu ? C::BP / 2 : C::BP;  // output columns of a tile
   int32_t* first = reinterpret_cast<int32_t*>(sm + 2 * C::stage);  // [E + 1] first tile of an expert
   int32_t* lists = reinterpret_cast<int32_t*>(sm + 2 * C::stage);  // of tokens, two for each gathered operand
-  first += ((GP ? 2 : 0) + (GQ ? 2 : 0)) * kList;
+  first += kLists<EPI, GP, GQ> * kList;
   float* probs = reinterpret_cast<float*>(first);  // of a tile's rows
   first += kProbs<C, EPI>;
   int32_t* begin = first + g.E + 1;                                // [E + 1] first row of an expert
@@ -666,42 +691,50 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
   };
   auto tokens = [&](const Where& w) {
     Tokens k;
-    if constexpr (EPI != kWeightGrad) {
+    if constexpr (EPI != kWeightGrad && GQ) {
 #pragma unroll
       for (int j = 0; j < LoaderQ::N; ++j)
-        if (g.q_token != nullptr) k.t[j] = g.q_token[w.r0 + min(LoaderQ::row(tid) + j * LoaderQ::RS, w.rows - 1)];
+        k.t[j] = g.q_token[w.r0 + min(LoaderQ::row(tid) + j * LoaderQ::RS, w.rows - 1)];
     }
     return k;
   };
+  // Rows of P's pieces (k inner): piece j lies far_p(j) rows from piece 0.  The gated activation takes 32
+  // gate rows and then the 32 up rows beside them (F rows on) for each wave.
+  auto far_p = [](int j) {
+    const int i = j * LoaderP::RS;
+    return EPI == kSwiglu ? (i >> 6) * 32 + (i & 31) : i;
+  };
+  auto up_p = [](int j) { return EPI == kSwiglu ? (j * LoaderP::RS >> 5) & 1 : 0; };
   auto start = [&](const Where& w, const Tokens& k) {
     const T* P = static_cast<const T*>(g.P);
     const T* Q = static_cast<const T*>(g.Q);
     if constexpr (EPI == kWeightGrad) {
       // an expert without rows may begin at the lists' end, where there is no token to look at
       const int32_t t0 = (int32_t)min((int64_t)w.r0, g.R - 1);
-      const int32_t* pt = g.p_token ? g.p_token + t0 : nullptr;
-      const int32_t* qt = g.q_token ? g.q_token + t0 : nullptr;
+      const int32_t* pt = GP ? g.p_token + t0 : nullptr;
+      const int32_t* qt = GQ ? g.q_token + t0 : nullptr;
       lp.start_outer(tid, w.rows, pt ? P : P + (int64_t)w.r0 * g.ldp, g.ldp, w.p0, g.Pd, pt, g.N - 1, lists);
       lq.start_outer(tid, w.rows, qt ? Q : Q + (int64_t)w.r0 * g.ldq, g.ldq, w.q0, g.Qd, qt, g.N - 1, lists + (GP ? 2 * kList : 0));
     } else {
       if constexpr (LP == kInner) {
-        // the gated activation takes 32 gate rows and the 32 up rows beside them for each wave
-        lp.start_inner(tid, g.K, P + (int64_t)w.e * (EPI == kSwiglu ? 2 * g.Pd : g.Pd) * g.ldp, g.ldp,
-                       [&](int i, int) {
-                         if constexpr (EPI == kSwiglu)
-                           return min(w.p0 + (i >> 6) * 32 + (i & 31), g.Pd - 1) + ((i >> 5) & 1) * g.Pd;
-                         else
-                           return min(w.p0 + i, g.Pd - 1);
-                       });
+        const T* we = P + (int64_t)w.e * (EPI == kSwiglu ? 2 * g.Pd : g.Pd) * g.ldp;
+        if constexpr (VEC)
+          lp.start_inner(tid, g.K, we, g.ldp, w.p0, g.Pd - 1);
+        else
+          lp.start_rows(tid, g.K, we, g.ldp, [&](int j) {
+            return min(w.p0 + LoaderP::row(tid) + far_p(j), g.Pd - 1) + up_p(j) * g.Pd;
+          });
       } else {
         lp.start_outer(tid, g.K, P + (int64_t)w.e * g.K * g.ldp, g.ldp, w.p0, g.Pd, nullptr, 0, nullptr);
       }
-      if (g.q_token != nullptr) {
+      if constexpr (GQ) {
         const uint32_t last = (uint32_t)g.N - 1u;
-        lq.start_inner(tid, g.K, Q, g.ldq, [&](int, int j) { return min((uint32_t)k.t[j], last); });
+        lq.start_rows(tid, g.K, Q, g.ldq, [&](int j) { return min((uint32_t)k.t[j], last); });
+      } else if constexpr (VEC) {
+        lq.start_inner(tid, g.K, Q + (int64_t)w.r0 * g.ldq, g.ldq, 0, w.rows - 1);
       } else {
-        lq.start_inner(tid, g.K, Q + (int64_t)w.r0 * g.ldq, g.ldq,
-                       [&](int i, int) { return min(i, w.rows - 1); });
+        lq.start_rows(tid, g.K, Q + (int64_t)w.r0 * g.ldq, g.ldq,
+                      [&](int j) { return min(LoaderQ::row(tid) + j * LoaderQ::RS, w.rows - 1); });
       }
     }
   };
@@ -727,10 +760,13 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
     constexpr int I = decltype(which)::value;
     const int at = load_slot * C::stage + (I < LoaderP::N ? 0 : C::BP * kStageBytes);
     auto one = [&](auto& l, auto piece) {
-      if constexpr (VEC)
-        l.template load<decltype(piece)::value>(tid, __builtin_amdgcn_readfirstlane(wave_lds + at));
+      constexpr int j = decltype(piece)::value;
+      if constexpr (!VEC)
+        l.template load<j>(tid, sm + at);
+      else if constexpr (I < LoaderP::N)
+        l.template load<j>(tid, __builtin_amdgcn_readfirstlane(wave_lds + at), far_p(j), up_p(j) * g.Pd * l.ldo);
       else
-        l.template load<decltype(piece)::value>(tid, sm + at);
+        l.template load<j>(tid, __builtin_amdgcn_readfirstlane(wave_lds + at), j * LoaderQ::RS, 0u);
     };
     if constexpr (I < LoaderP::N)
       one(lp, std::integral_constant<int, I>{});
@@ -784,7 +820,7 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
     for (int j = 0; j < C::MQ; ++j) f.q[j] = rq.get(sq, j, s);
   };
 
-  if constexpr (GP || GQ) {  // the first lists
+  if constexpr (kLists<EPI, GP, GQ> > 0) {  // the first lists
     wait_memory<0>();
     wave_barrier();
   }
@@ -894,10 +930,7 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
               m = max(m, (uint32_t)__shfl_xor((int)m, 2));
               const uint32_t byte = act8_exponent(m);
               const float inv = act8_inverse(byte);
-              v2u q = v2u{0u, 0u};
-#pragma unroll
-              for (int v = 0; v < 8; ++v)
-                q[v >> 2] |= ((uint32_t)act8_round(a[half][v], inv, byte) & 255u) << (8 * (v & 3));
+              const v2u q = v2u{act8_round4(a[half], inv, byte), act8_round4(a[half] + 4, inv, byte)};
               if (live && n > 0) {
                 int8_t* d = g.q8 + (r * 2 + half) * F + f0 + c;
                 if (g.vec_q8) {
@@ -971,16 +1004,17 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
             const float sg = act8_scale((uint32_t)__shfl((int)k.e, row * 4 + (c >> 5)));
             const float su = act8_scale((uint32_t)__shfl((int)k.e, row * 4 + 2 + (c >> 5)));
             const float p = probs[rr];
-            float dp = 0.0f;
+            float dp = 0.0f, gate[4], up[4];
+            act8_values4(qg, sg, gate);
+            act8_values4(qu, su, up);
             v4f dg, du, hv;
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
-              const float gt = (float)(int8_t)(qg >> (8 * v)) * sg, up = (float)(int8_t)(qu >> (8 * v)) * su;
-              const float z = sigmoid(gt), sl = gt * z, ds = p * dh[v];
-              dp += v < n ? dh[v] * (sl * up) : 0.0f;
-              hv[v] = p * (sl * up);
+              const float z = sigmoid(gate[v]), sl = gate[v] * z, act = sl * up[v], ds = p * dh[v];
+              dp += v < n ? dh[v] * act : 0.0f;
+              hv[v] = p * act;
               du[v] = ds * sl;
-              dg[v] = ds * up * (z * (1.0f + gt * (1.0f - z)));
+              dg[v] = ds * up[v] * (z + sl * (1.0f - z));
             }
             if (rr < w.rows && n > 0) {
               T* da = static_cast<T*>(g.out) + r * 2 * F + f0 + c;
@@ -1006,7 +1040,7 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
 template <typename T, typename C, int LP, int LQ, int EPI, int LOAD, bool GP = false, bool GQ = false>
 hipError_t launch_gemm(const ExpertGemm& g, hipStream_t s) {
   const void* kern = reinterpret_cast<const void*>(k_expert_gemm<T, C, LP, LQ, EPI, LOAD, GP, GQ>);
-  const size_t lds = 2 * (size_t)C::stage + (((GP ? 2 : 0) + (GQ ? 2 : 0)) * kList + kProbs<C, EPI>) * 4 + (size_t)(g.E + 1) * 8;
+  const size_t lds = 2 * (size_t)C::stage + (kLists<EPI, GP, GQ> * kList + kProbs<C, EPI>) * 4 + (size_t)(g.E + 1) * 8;
   hipError_t e = hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
   if (e != hipSuccess) return e;
   int occ = 0;
@@ -1026,13 +1060,25 @@ hipError_t launch_gemm(const ExpertGemm& g, hipStream_t s) {
 
 // big: the large tile.  Operands that are not whole pieces go element by element; rows by token
 // that span 4 GiB or more take wide offsets, on the small tile.
-// GP, GQ: k-outer rows of P and Q are taken by token (an element loader looks at the list itself).
+// GP, GQ: rows of P and Q are taken by token.
 template <typename T, int LP, int LQ, int EPI, bool GP = false, bool GQ = false>
 hipError_t pick_gemm(const ExpertGemm& g, bool big, bool vec, hipStream_t s) {
   if (!vec)
-    return big ? launch_gemm<T, Big, LP, LQ, EPI, kElements>(g, s) : launch_gemm<T, Small, LP, LQ, EPI, kElements>(g, s);
-  if (g.wide) return launch_gemm<T, Small, LP, LQ, EPI, kWidePieces, GP, GQ>(g, s);
+    return big ? launch_gemm<T, Big, LP, LQ, EPI, kElements, GP, GQ>(g, s)
+               : launch_gemm<T, Small, LP, LQ, EPI, kElements, GP, GQ>(g, s);
+  if constexpr (GP || GQ) {
+    if (g.wide) return launch_gemm<T, Small, LP, LQ, EPI, kWidePieces, GP, GQ>(g, s);
+  }
   return big ? launch_gemm<T, Big, LP, LQ, EPI, kPieces, GP, GQ>(g, s) : launch_gemm<T, Small, LP, LQ, EPI, kPieces, GP, GQ>(g, s);
+}
+
+// Large tiles for bf16 where an expert has rows for them on average, small ones
+// else: fp32's matrix instructions take 16 times as long, so that a small tile's
+// loads are hidden too, and it wastes less at the end of an expert's rows and of
+// the tile list (49,146 rows 1,536 -> 1,024 of 48 experts: 1,298 us against 1,468).
+template <typename T>
+bool big_tiles(const ExpertGemm& g) {
+  return sizeof(T) == 2 && g.R / g.E >= 128;
 }
 
 }  // namespace expert

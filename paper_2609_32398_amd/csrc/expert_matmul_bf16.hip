@@ -1,0 +1,18 @@
+// Products of rows with their expert's weights, and with the transposed weights, bf16.
+#include <algorithm>
+
+#include "expert_gemm.h"
+
+namespace dol {
+
+hipError_t launch_expert_matmul_bf16(const ExpertGemm& g, bool transposed, bool vec, hipStream_t s) {
+  using namespace expert;
+  const bool big = big_tiles<uint16_t>(g);
+  if (g.q_token != nullptr)
+    return transposed ? pick_gemm<uint16_t, kOuter, kInner, kStore, false, true>(g, big, vec, s)
+                      : pick_gemm<uint16_t, kInner, kInner, kStore, false, true>(g, big, vec, s);
+  return transposed ? pick_gemm<uint16_t, kOuter, kInner, kStore>(g, big, vec, s)
+                    : pick_gemm<uint16_t, kInner, kInner, kStore>(g, big, vec, s);
+}
+
+}  // namespace dol

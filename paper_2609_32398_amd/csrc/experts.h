@@ -53,7 +53,8 @@ struct ExpertGemm {
   float* dp;               // backward pass: partial sums of the probabilities' gradient, [R][ceil(F / 64)]
 };
 
-hipError_t launch_expert_matmul(const ExpertGemm& g, do_dtype dt, bool transposed, bool vec, hipStream_t s);
+hipError_t launch_expert_matmul_bf16(const ExpertGemm& g, bool transposed, bool vec, hipStream_t s);
+hipError_t launch_expert_matmul_f32(const ExpertGemm& g, bool transposed, bool vec, hipStream_t s);
 hipError_t launch_expert_weight_grad_bf16(const ExpertGemm& g, bool big, bool vec, hipStream_t s);
 hipError_t launch_expert_weight_grad_f32(const ExpertGemm& g, bool big, bool vec, hipStream_t s);
 hipError_t launch_expert_swiglu(const ExpertGemm& g, do_dtype dt, bool vec, hipStream_t s);
@@ -94,9 +95,21 @@ __device__ __forceinline__ float act8_inverse(uint32_t byte) {
 __device__ __forceinline__ float act8_scale(uint32_t byte) {
   return byte == 255u ? __uint_as_float(0x7FC00000u) : __uint_as_float(byte << 23);
 }
-// x * 2^-e to the nearest integer, ties to even: x * 2^-e is exact (or so small that it rounds to 0).
-__device__ __forceinline__ int act8_round(float x, float inv, uint32_t byte) {
-  return byte == 255u ? 0 : (int)__builtin_rintf(x * inv);
+// Four values x * 2^-e to the nearest integers, ties to even, one to a byte (x 2^-e
+// is exact, or so small that it rounds to 0).  fma(x, 2^-e, 1.5 * 2^23) rounds
+// once, at the unit, and its low byte is the integer in two's complement.
+__device__ __forceinline__ uint32_t act8_round4(const float* x, float inv, uint32_t byte) {
+  uint32_t b[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) b[i] = __float_as_uint(__builtin_fmaf(x[i], inv, 12582912.0f));
+  const uint32_t lo = __builtin_amdgcn_perm(b[1], b[0], 0x0C0C0400u), hi = __builtin_amdgcn_perm(b[3], b[2], 0x04000C0Cu);
+  return byte == 255u ? 0u : lo | hi;
+}
+// Four 8-bit values times s = 2^e, exactly.
+__device__ __forceinline__ void act8_values4(uint32_t q, float s, float* v) {
+  const uint32_t u = q ^ 0x80808080u;  // + 128: unsigned bytes convert in one instruction
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = ((float)((u >> (8 * i)) & 255u) - 128.0f) * s;
 }
 
 }  // namespace dol
