@@ -298,8 +298,10 @@ struct PieceLoader {
   }
 };
 
-// The same for rows of any width and alignment, element by element through
-// registers.
+// The same for rows of any width and alignment, through registers.  A piece is 16
+// bytes from wherever its first element lies (global memory takes any alignment),
+// elements past the row's end zeroed; only a wave that would read past the
+// operand's own end takes its pieces element by element.
 template <typename T, int LAYOUT, int DIM, int THREADS>
 struct ElementLoader {
   static constexpr int EL = Mma<T>::kElems;
@@ -307,10 +309,14 @@ struct ElementLoader {
   static constexpr int N = DIM * kStageBytes / 16 / THREADS;
   static constexpr int PR = LAYOUT == kInner ? kStageBytes / 16 : DIM / EL;
   static constexpr int RS = THREADS / PR;
-  const T* ptr[N];
-  int32_t k;     // first k of the thread's next pieces (k inner: of the piece)
+  static constexpr int G = 4;  // pieces that are loaded together
+  static_assert(N % G == 0);
+  const T* ptr[LAYOUT == kInner ? N : 1];
+  const T* first;  // the operand, and its end
+  const T* end;
+  int32_t k;       // first k of the thread's next pieces (k inner: of the piece)
   int32_t K;
-  int32_t cols;  // k outer: elements of the row from the piece on
+  int32_t cols;    // k outer: elements of the row from the piece on
   int64_t ld;
   const int32_t* token;
   const T* base;
@@ -323,6 +329,10 @@ struct ElementLoader {
       return slot ^ inner_swizzle(row(tid));
     else
       return slot ^ outer_swizzle<T, DIM>(row(tid));
+  }
+  __device__ __forceinline__ void bounds(const void* p, int64_t elements) {
+    first = static_cast<const T*>(p);
+    end = first + elements;
   }
   template <typename F>
   __device__ __forceinline__ void start_rows(int tid, int32_t K_, const T* b, int32_t ld_, F&& rowi) {
@@ -342,28 +352,59 @@ struct ElementLoader {
     cols = cols_ - c;
     base = b + (cols > 0 ? c : 0);
   }
+  // Pieces J .. J + G - 1 of the stage at dst.
   template <int J>
   __device__ __forceinline__ void load(int tid, char* dst) {
-    const int kk = LAYOUT == kInner ? k : k + J * RS;
-    const int n = kk >= K ? 0 : (LAYOUT == kInner ? K - kk : cols);  // elements that exist
-    const T* src = ptr[J];
-    if constexpr (LAYOUT == kOuter) {
-      int64_t r = kk;
-      if (token != nullptr && kk < K) {
-        r = token[kk];
-        r = r < 0 || r > last ? last : r;
-      }
-      src = base + r * ld;
-    }
-    union {
-      T el[EL];
-      v4u v;
-    } u;
-    u.v = v4u{0u, 0u, 0u, 0u};
+    const T* src[G];
+    int n[G];  // elements that exist
+    bool part = false, past = first + EL > end;
 #pragma unroll
-    for (int i = 0; i < EL; ++i)
-      if (i < n) u.el[i] = src[i];
-    *reinterpret_cast<v4u*>(dst + (tid + J * THREADS) * 16) = u.v;
+    for (int i = 0; i < G; ++i) {
+      if constexpr (LAYOUT == kInner) {
+        n[i] = K - k;
+        src[i] = ptr[J + i];
+      } else {
+        const int kk = k + (J + i) * RS;
+        n[i] = kk < K ? cols : 0;
+        int64_t r = kk;
+        if (token != nullptr && kk < K) {
+          r = token[kk];
+          r = r < 0 || r > last ? last : r;
+        }
+        src[i] = base + r * ld;
+      }
+      part |= n[i] < EL;
+      past |= n[i] > 0 && src[i] + EL > end;
+    }
+    v4u v[G];
+    if (__ballot(past) == 0) {
+#pragma unroll
+      for (int i = 0; i < G; ++i) __builtin_memcpy(&v[i], n[i] > 0 ? src[i] : first, 16);
+      if (__ballot(part) != 0) {
+#pragma unroll
+        for (int i = 0; i < G; ++i)
+#pragma unroll
+          for (int d = 0; d < 4; ++d) {
+            const int bits = min(32, max(0, n[i] * (int)sizeof(T) * 8 - 32 * d));
+            v[i][d] &= bits == 32 ? ~0u : (1u << bits) - 1u;
+          }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < G; ++i) {
+        v[i] = v4u{0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int e = 0; e < EL; ++e)
+          if (e < n[i]) {
+            if constexpr (sizeof(T) == 2)
+              v[i][e >> 1] |= (uint32_t)src[i][e] << (16 * (e & 1));
+            else
+              v[i][e] = __float_as_uint(src[i][e]);
+          }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < G; ++i) *reinterpret_cast<v4u*>(dst + (tid + (J + i) * THREADS) * 16) = v[i];
   }
   __device__ __forceinline__ void next(int) {
     k += KS;
@@ -685,6 +726,16 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
     w.nk = max(1, (w.have + KS - 1) / KS);
     return w;
   };
+  if constexpr (!VEC) {
+    // elements of the operands
+    if constexpr (EPI == kWeightGrad) {
+      lp.bounds(g.P, (GP ? g.N : g.R) * g.ldp);
+      lq.bounds(g.Q, (GQ ? g.N : g.R) * g.ldq);
+    } else {
+      lp.bounds(g.P, (int64_t)g.E * (LP == kOuter ? g.K : (EPI == kSwiglu ? 2 : 1) * g.Pd) * g.ldp);
+      lq.bounds(g.Q, (GQ ? g.N : g.R) * g.ldq);
+    }
+  }
   // the tokens of a thread's rows of a tile, loaded ahead of start()
   struct Tokens {
     int32_t t[LoaderQ::N];
@@ -761,12 +812,14 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
     const int at = load_slot * C::stage + (I < LoaderP::N ? 0 : C::BP * kStageBytes);
     auto one = [&](auto& l, auto piece) {
       constexpr int j = decltype(piece)::value;
-      if constexpr (!VEC)
-        l.template load<j>(tid, sm + at);
-      else if constexpr (I < LoaderP::N)
+      if constexpr (!VEC) {
+        if constexpr (j % 4 == 0) l.template load<j>(tid, sm + at);  // four together
+      } else if constexpr (I < LoaderP::N)
+        {
         l.template load<j>(tid, __builtin_amdgcn_readfirstlane(wave_lds + at), far_p(j), up_p(j) * g.Pd * l.ldo);
-      else
+      } else {
         l.template load<j>(tid, __builtin_amdgcn_readfirstlane(wave_lds + at), j * LoaderQ::RS, 0u);
+      }
     };
     if constexpr (I < LoaderP::N)
       one(lp, std::integral_constant<int, I>{});
