@@ -58,9 +58,27 @@ do_status check_widths(int64_t R, int32_t E, std::initializer_list<int32_t> w) {
     return set_error(DO_ERR_OVERFLOW, "too many rows for rows of this width");
   return DO_OK;
 }
+
 // An operand of whole 16-byte pieces: its address and the length of its rows, and fewer than 2^32 pieces.
 bool whole(const void* p, do_dtype dt, int32_t row, int64_t rows = 1) {
   return aligned(p, 16) && row * size_of(dt) % 16 == 0 && rows * (int64_t)(row * size_of(dt) / 16) < (int64_t(1) << 32);
+}
+
+// The same for weights whose rows are read along: one expert's byte offsets fit 32 bits too.
+bool whole_expert(const void* w, do_dtype dt, int32_t row, int64_t rows) {
+  return whole(w, dt, row) && rows * row * (int64_t)size_of(dt) < (int64_t(1) << 32);
+}
+
+// Whether there are few rows, and the experts that can have them are so few that their tiles of `cols`
+// weight rows leave CUs idle, or, in fp32, whose matrix instructions take 16 times as long, fill them less than twice: then a
+// tile's time counts, and it is shorter with a quarter of the contraction for each wave.  Against the
+// tiles that share LDS, 8 experts a token, 768 -> 2,048 and gated 2,048 -> 2 x 768: bf16, 1 token 16.7 and
+// 19.4 us against 16.7 and 24.7 (within the rule), 4 tokens 26.0 and 44.4 against 17.7 and 41.0 (outside);
+// fp32, 1 token 17.6 and 32.6 against 34.2 and 84.8, 4 tokens 43.1 and 79.3 against 56.9 and 142.9
+// (within), 16 tokens 90.1 and 158 against 89.8 and 149 (outside).
+bool few_tiles(do_dtype dt, int64_t R, int32_t E, int32_t width, int cols) {
+  const int64_t tiles = std::min<int64_t>(R, E) * ((width + cols - 1) / cols);
+  return dol::few_rows(R, E) && tiles <= (dt == DO_F32 ? 2 : 1) * dol::device_info().cu_count;
 }
 
 // Rows taken by token whose byte offsets pass 32 bits.
@@ -132,8 +150,11 @@ DOLOSS_API do_status do_expert_matmul(const void* x, const void* w, do_dtype dty
   g.out = y;
   g.wide = row_token != nullptr && wide(dtype, in, N);
   g.vec_out = whole(y, dtype, out);
+  const bool vec = (transposed ? whole(w, dtype, I) : whole_expert(w, dtype, I, O)) &&
+                   whole(x, dtype, in, row_token != nullptr ? N : R);
+  if (vec && !transposed && few_tiles(dtype, R, E, O, 128)) return launched(dol::launch_expert_skinny(g, dtype, false, stream));
   return launched((dtype == DO_F32 ? dol::launch_expert_matmul_f32 : dol::launch_expert_matmul_bf16)(
-      g, transposed != 0, whole(w, dtype, I) && whole(x, dtype, in, row_token != nullptr ? N : R), stream));
+      g, transposed != 0, vec, stream));
 }
 
 DOLOSS_API do_status do_expert_weight_grad(const void* dy, const void* x, do_dtype dtype, const int32_t* offsets,
@@ -221,7 +242,9 @@ DOLOSS_API do_status do_expert_swiglu(const void* x, const void* w1, do_dtype dt
   g.out = h;
   g.vec_out = aligned(h, 16) && F % 8 == 0;
   g.vec_q8 = q != nullptr && aligned(q, 8) && F % 8 == 0;
-  return launched(dol::launch_expert_swiglu(g, dtype, whole(x, dtype, H, N) && whole(w1, dtype, H), stream));
+  const bool vec = whole(x, dtype, H, N) && whole_expert(w1, dtype, H, 2 * (int64_t)F);
+  if (vec && few_tiles(dtype, R, E, F, 64)) return launched(dol::launch_expert_skinny(g, dtype, true, stream));
+  return launched(dol::launch_expert_swiglu(g, dtype, vec, stream));
 }
 
 DOLOSS_API int64_t do_expert_swiglu_grad_workspace(int64_t R, int32_t F) {

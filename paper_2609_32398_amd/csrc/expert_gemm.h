@@ -18,7 +18,7 @@
 // A stage is 128 bytes of k for an operand row (k inner), or that many rows of k
 // (k outer), in LDS, double buffered: while a stage is multiplied the next one is
 // loaded, across tiles too.  Half of the waves, one on each SIMD, issue all loads
-// of a stage: the vector cache holds no more than 32 KiB on their way, so that
+// of a stage (both of a two-wave block's): the vector cache holds no more than 32 KiB on their way, so that
 // the issue of a stage's 64 KiB takes about half of its time, in which the other
 // wave of the SIMD multiplies.
 // A 16-byte piece of a stage lies at a place XOR-ed with its row, so that the
@@ -27,6 +27,7 @@
 // lane that is permuted.
 #pragma once
 
+#include <atomic>
 #include <type_traits>
 
 #include "experts.h"
@@ -47,6 +48,7 @@ enum { kElements = 0, kPieces = 1, kWidePieces = 2 };  // how the operands are l
 enum { kStore = 0, kWeightGrad = 1, kSwiglu = 2, kSwigluGrad = 3 };
 
 constexpr int kStageBytes = 128;  // of k for one operand row
+constexpr size_t kLdsBytes = 160 << 10;  // of a CU
 constexpr int kList = 1024;       // tokens of a list in LDS
 constexpr int kPhases = 4;        // of a stage: a quarter of its k each
 
@@ -55,7 +57,7 @@ template <int BP_, int BQ_, int WP_, int WQ_, int OCC_>
 struct Tile {
   static constexpr int BP = BP_, BQ = BQ_, WP = WP_, WQ = WQ_;
   static constexpr int waves = WP * WQ, threads = waves * kWave;
-  static constexpr int loaders = threads / 2;                 // threads that load
+  static constexpr int loaders = waves == 2 ? threads : threads / 2;  // threads that load
   static constexpr int MP = BP / WP / 32, MQ = BQ / WQ / 32;  // 32 x 32 matrix tiles of a wave
   static constexpr int stage = (BP + BQ) * kStageBytes;
   static constexpr int occ = OCC_;  // waves per SIMD to leave registers for
@@ -64,6 +66,7 @@ struct Tile {
 };
 using Big = Tile<256, 256, 4, 2, 2>;
 using Small = Tile<128, 64, 2, 2, 2>;
+using Few = Tile<128, 32, 2, 1, 2>;
 
 template <typename T>
 struct Mma;
@@ -169,7 +172,8 @@ struct PieceLoader {
   static constexpr int PR = LAYOUT == kInner ? kStageBytes / 16 : DIM / EL;  // pieces of an LDS row
   static constexpr int RS = THREADS / PR;                     // LDS rows between a thread's pieces
   static constexpr uint32_t kUnit = WIDE ? EL : 1, kBytes = WIDE ? 1 : sizeof(T);  // elements / kUnit * kBytes: offsets
-  static_assert(LAYOUT == kInner || (kWave % PR == 0 && (sizeof(T) == 4 || RS % 4 == 0)));
+  // a thread's pieces share their XOR
+  static_assert(LAYOUT == kInner ? RS % 16 == 0 : kWave % PR == 0 && (sizeof(T) == 4 || RS % 4 == 0));
   const char* base;  // of the stage
   int64_t step;      // bytes to the next stage
   int32_t left;      // k from the stage's first on
@@ -792,7 +796,7 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
   const uint32_t wave_lds = (uint32_t)(uintptr_t)(DOL_LDS char*)sm + (uint32_t)(tid & ~63) * 16;
 
   // The loaders run a stage ahead of the products, through the tiles in the same order.
-  const bool loader = wave < C::waves / 2;
+  const bool loader = tid < C::loaders;
   Where wl = locate(tile);
   int load_tile = tile, load_left = wl.nk, load_slot = 0;
   int32_t load_have = wl.have, have = wl.have;  // k from the next stage's first on, and from the last loaded one's
@@ -814,8 +818,7 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
       constexpr int j = decltype(piece)::value;
       if constexpr (!VEC) {
         if constexpr (j % 4 == 0) l.template load<j>(tid, sm + at);  // four together
-      } else if constexpr (I < LoaderP::N)
-        {
+      } else if constexpr (I < LoaderP::N) {
         l.template load<j>(tid, __builtin_amdgcn_readfirstlane(wave_lds + at), far_p(j), up_p(j) * g.Pd * l.ldo);
       } else {
         l.template load<j>(tid, __builtin_amdgcn_readfirstlane(wave_lds + at), j * LoaderQ::RS, 0u);
@@ -895,11 +898,11 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
 #pragma unroll
         for (int i = 0; i < C::MP; ++i) acc[i][j] = Mma<T>::mul(f.p[i], f.q[j], acc[i][j]);
     };
-    // A tile's row probabilities: loaded now by the waves that load nothing else (a wait for them would
-    // include all loads before), used after the last stage.
+    // A tile's row probabilities: loaded now, by waves that load nothing else where there are some (a wait
+    // for them would include all loads before), used after the last stage.
     float prob = 0.0f;
     const int prob_row = tid - (C::threads - C::loaders);
-    static_assert(kProbs<C, EPI> <= C::threads - C::loaders);
+    static_assert(kProbs<C, EPI> <= C::loaders);
     if (kProbs<C, EPI> > 0 && prob_row >= 0 && prob_row < w.rows && prob_row < C::BQ)
       prob = row_prob(g, w.r0 + prob_row, w.e);
     for (int ks = 0; ks < w.nk; ++ks) {
@@ -909,7 +912,7 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
       }
       wave_barrier();
       if (loader) load_stage();
-      #pragma unroll
+#pragma unroll
       for (int s = 0; s < kPhases; ++s) {
         Frags f;
         read(f, buf, s);
@@ -1093,45 +1096,73 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
 template <typename T, typename C, int LP, int LQ, int EPI, int LOAD, bool GP = false, bool GQ = false>
 hipError_t launch_gemm(const ExpertGemm& g, hipStream_t s) {
   const void* kern = reinterpret_cast<const void*>(k_expert_gemm<T, C, LP, LQ, EPI, LOAD, GP, GQ>);
-  const size_t lds = 2 * (size_t)C::stage + (kLists<EPI, GP, GQ> * kList + kProbs<C, EPI>) * 4 + (size_t)(g.E + 1) * 8;
-  hipError_t e = hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-  if (e != hipSuccess) return e;
-  int occ = 0;
-  if ((e = hipOccupancyMaxActiveBlocksPerMultiprocessor(&occ, kern, C::threads, lds)) != hipSuccess) return e;
-  if (occ < 1) return hipErrorLaunchOutOfResources;
+  auto lds_of = [](int E) {
+    return 2 * (size_t)C::stage + (kLists<EPI, GP, GQ> * kList + kProbs<C, EPI>) * 4 + (size_t)(E + 1) * 8;
+  };
+  // blocks per CU that the registers leave room for, and the kernel's LDS limit: set up once per device
+  static std::atomic<int> by_registers[64];
+  const DevInfo di = device_info();
+  if (di.device < 0 || di.device >= 64) return hipErrorInvalidDevice;
+  int occ = by_registers[di.device].load(std::memory_order_acquire);
+  if (occ == 0) {
+    hipError_t e = hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds_of(kMaxE));
+    if (e != hipSuccess) return e;
+    if ((e = hipOccupancyMaxActiveBlocksPerMultiprocessor(&occ, kern, C::threads, 0)) != hipSuccess) return e;
+    if (occ < 1) return hipErrorLaunchOutOfResources;
+    by_registers[di.device].store(occ, std::memory_order_release);
+  }
+  const size_t lds = lds_of(g.E);
+  occ = std::max(1, std::min<int>(occ, (int)(kLdsBytes / lds)));
   constexpr int BPo = EPI == kSwiglu ? C::BP / 2 : C::BP;
   const int64_t PT = (g.Pd + BPo - 1) / BPo;
   // at most this many tiles (the experts' row counts are only known on the device)
   const int64_t tiles = EPI == kWeightGrad ? (int64_t)g.E * PT * ((g.Qd + C::BQ - 1) / C::BQ)
                                            : PT * (g.R / C::BQ + std::min<int64_t>(g.E, g.R));
   if (tiles >= (int64_t(1) << 31)) return hipErrorInvalidValue;
-  const int64_t blocks = std::min<int64_t>((tiles + 7) & ~int64_t(7), (int64_t)occ * device_info().cu_count & ~int64_t(7));
+  const int64_t blocks = std::min<int64_t>((tiles + 7) & ~int64_t(7), (int64_t)occ * di.cu_count & ~int64_t(7));
   hipLaunchKernelGGL((k_expert_gemm<T, C, LP, LQ, EPI, LOAD, GP, GQ>), dim3((unsigned)std::max<int64_t>(8, blocks)),
                      dim3(C::threads), lds, s, g);
   return hipGetLastError();
 }
 
-// big: the large tile.  Operands that are not whole pieces go element by element; rows by token
+// The tile by its size.  Operands that are not whole pieces go through registers; rows by token
 // that span 4 GiB or more take wide offsets, on the small tile.
 // GP, GQ: rows of P and Q are taken by token.
+enum { kFew = 0, kSmall = 1, kBig = 2 };
 template <typename T, int LP, int LQ, int EPI, bool GP = false, bool GQ = false>
-hipError_t pick_gemm(const ExpertGemm& g, bool big, bool vec, hipStream_t s) {
-  if (!vec)
-    return big ? launch_gemm<T, Big, LP, LQ, EPI, kElements, GP, GQ>(g, s)
-               : launch_gemm<T, Small, LP, LQ, EPI, kElements, GP, GQ>(g, s);
+hipError_t pick_gemm(const ExpertGemm& g, int size, bool vec, hipStream_t s) {
   if constexpr (GP || GQ) {
-    if (g.wide) return launch_gemm<T, Small, LP, LQ, EPI, kWidePieces, GP, GQ>(g, s);
+    if (vec && g.wide) return launch_gemm<T, Small, LP, LQ, EPI, kWidePieces, GP, GQ>(g, s);
   }
-  return big ? launch_gemm<T, Big, LP, LQ, EPI, kPieces, GP, GQ>(g, s) : launch_gemm<T, Small, LP, LQ, EPI, kPieces, GP, GQ>(g, s);
+  if constexpr (EPI != kWeightGrad) {
+    if (vec && size == kFew) return launch_gemm<T, Few, LP, LQ, EPI, kPieces, GP, GQ>(g, s);
+  }
+  if constexpr (EPI == kWeightGrad || sizeof(T) == 2) {
+    if (size == kBig)
+      return vec ? launch_gemm<T, Big, LP, LQ, EPI, kPieces, GP, GQ>(g, s)
+                 : launch_gemm<T, Big, LP, LQ, EPI, kElements, GP, GQ>(g, s);
+  }
+  return vec ? launch_gemm<T, Small, LP, LQ, EPI, kPieces, GP, GQ>(g, s)
+             : launch_gemm<T, Small, LP, LQ, EPI, kElements, GP, GQ>(g, s);
 }
 
-// Large tiles for bf16 where an expert has rows for them on average, small ones
-// else: fp32's matrix instructions take 16 times as long, so that a small tile's
-// loads are hidden too, and it wastes less at the end of an expert's rows and of
-// the tile list (49,146 rows 1,536 -> 1,024 of 48 experts: 1,298 us against 1,468).
+// Tiles of rows by the experts' rows on average.
+//
+// 16 or fewer: half as many rows as the small tile, all waves load.  A stage is 20
+// KiB, so that a CU's blocks have more of the weights on their way, which bound
+// the time (5.4 TB/s of weights).  8 of 64 experts a token, fp32, 768 -> 2,048 and
+// gated 2,048 -> 2 x 768, against the small tile: 8 rows an expert 90 and 156 us
+// against 114 and 218, 16 rows 91 and 160 against 98 and 167; 32 rows 116 and 285
+// against 126 and 225, since half of the experts then need two tiles.
+//
+// Large tiles for bf16 where an expert has rows for them, small ones else: fp32's
+// matrix instructions take 16 times as long, so that a small tile's loads are
+// hidden too, and it wastes less at the end of an expert's rows and of the tile
+// list (49,146 rows 1,536 -> 1,024 of 48 experts: 1,298 us against 1,468).
 template <typename T>
-bool big_tiles(const ExpertGemm& g) {
-  return sizeof(T) == 2 && g.R / g.E >= 128;
+int tile_size(const ExpertGemm& g) {
+  if (few_rows(g.R, g.E)) return kFew;
+  return sizeof(T) == 2 && g.R / g.E >= 128 ? kBig : kSmall;
 }
 
 }  // namespace expert

@@ -7,12 +7,12 @@ namespace dol {
 
 hipError_t launch_expert_matmul_bf16(const ExpertGemm& g, bool transposed, bool vec, hipStream_t s) {
   using namespace expert;
-  const bool big = big_tiles<uint16_t>(g);
+  const int size = tile_size<uint16_t>(g);
   if (g.q_token != nullptr)
-    return transposed ? pick_gemm<uint16_t, kOuter, kInner, kStore, false, true>(g, big, vec, s)
-                      : pick_gemm<uint16_t, kInner, kInner, kStore, false, true>(g, big, vec, s);
-  return transposed ? pick_gemm<uint16_t, kOuter, kInner, kStore>(g, big, vec, s)
-                    : pick_gemm<uint16_t, kInner, kInner, kStore>(g, big, vec, s);
+    return transposed ? pick_gemm<uint16_t, kOuter, kInner, kStore, false, true>(g, size, vec, s)
+                      : pick_gemm<uint16_t, kInner, kInner, kStore, false, true>(g, size, vec, s);
+  return transposed ? pick_gemm<uint16_t, kOuter, kInner, kStore>(g, size, vec, s)
+                    : pick_gemm<uint16_t, kInner, kInner, kStore>(g, size, vec, s);
 }
 
 }  // namespace dol

@@ -7,11 +7,12 @@ namespace dol {
 
 hipError_t launch_expert_weight_grad_f32(const ExpertGemm& g, bool big, bool vec, hipStream_t s) {
   using namespace expert;
+  const int size = big ? kBig : kSmall;
   const bool p = g.p_token != nullptr, q = g.q_token != nullptr;
-  if (p && q) return pick_gemm<float, kOuter, kOuter, kWeightGrad, true, true>(g, big, vec, s);
-  if (p) return pick_gemm<float, kOuter, kOuter, kWeightGrad, true, false>(g, big, vec, s);
-  if (q) return pick_gemm<float, kOuter, kOuter, kWeightGrad, false, true>(g, big, vec, s);
-  return pick_gemm<float, kOuter, kOuter, kWeightGrad>(g, big, vec, s);
+  if (p && q) return pick_gemm<float, kOuter, kOuter, kWeightGrad, true, true>(g, size, vec, s);
+  if (p) return pick_gemm<float, kOuter, kOuter, kWeightGrad, true, false>(g, size, vec, s);
+  if (q) return pick_gemm<float, kOuter, kOuter, kWeightGrad, false, true>(g, size, vec, s);
+  return pick_gemm<float, kOuter, kOuter, kWeightGrad>(g, size, vec, s);
 }
 
 }  // namespace dol

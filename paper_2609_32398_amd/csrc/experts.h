@@ -59,6 +59,10 @@ hipError_t launch_expert_weight_grad_bf16(const ExpertGemm& g, bool big, bool ve
 hipError_t launch_expert_weight_grad_f32(const ExpertGemm& g, bool big, bool vec, hipStream_t s);
 hipError_t launch_expert_swiglu(const ExpertGemm& g, do_dtype dt, bool vec, hipStream_t s);
 hipError_t launch_expert_swiglu_grad(const ExpertGemm& g, do_dtype dt, bool vec, hipStream_t s);
+// 16 rows an expert or fewer on average.
+inline bool few_rows(int64_t R, int32_t E) { return R / E <= 16; }
+// Forward products (swiglu: with the gated activation) of whole pieces for few rows per expert.
+hipError_t launch_expert_skinny(const ExpertGemm& g, do_dtype dt, bool swiglu, hipStream_t s);
 // dp [N][E] (fp32 or bf16) from the partial sums: zero where a token has no row.
 hipError_t launch_expert_dp(const float* part, int32_t nparts, int64_t R, const int32_t* token_row,
                             const int32_t* token_expert, int64_t N, int32_t k, int32_t E, void* dp, do_dtype dt,

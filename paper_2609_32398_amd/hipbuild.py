@@ -10,7 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "libdoloss.so")
 SOURCES = ["api.hip", "topk.hip", "topk_ragged.hip", "topk_pieces.hip", "topk_wide.hip", "reduce.hip", "surrogate.hip", "loadstats.hip", "rem.hip",
-           "expert_api.hip", "expert_rows.hip", "expert_matmul_bf16.hip", "expert_matmul_f32.hip", "expert_wgrad_bf16.hip", "expert_wgrad_f32.hip", "expert_swiglu.hip", "act8.hip"]
+           "expert_api.hip", "expert_rows.hip", "expert_matmul_bf16.hip", "expert_matmul_f32.hip", "expert_wgrad_bf16.hip", "expert_wgrad_f32.hip", "expert_swiglu.hip", "expert_skinny.hip", "act8.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950",
