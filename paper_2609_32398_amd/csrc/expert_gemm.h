@@ -25,6 +25,14 @@
 // matrix operands are read from LDS without bank conflicts; the loads that go
 // straight to LDS write it in lane order, so it is the global address of each
 // lane that is permuted.
+//
+// 65,536 tokens of 8 of 128 experts (524,288 rows), bf16: 768 -> 2,048 in 1,680 us
+// (980 TFLOP/s), weight gradient of 1,536 x 2,048 in 3,530 us (940), 2,048 -> 2 x
+// 768 with the gated activation and its checkpoint in 3,330 us (990).  The matrix
+// cores are busy 55 % of the time at the clock of about 2 GHz that they leave; the
+// rest is the loads' way through the vector cache (a stage takes it 1.4 us, its
+// products 1.0) and the outputs at a tile's end.  fp32, 49,146 rows 1,536 -> 1,024
+// transposed: 1,260 us, 123 of the 155 TFLOP/s of a large matrix product.
 #pragma once
 
 #include <atomic>
