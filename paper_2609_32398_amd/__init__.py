@@ -124,7 +124,8 @@ def _check(status: int, where: str):
 
 
 def _stream() -> ctypes.c_void_p:
-    return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    # the handle alone: 0.4 us, where a torch.cuda.Stream around it takes 3
+    return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
 
 
 def _dtype_code(t: torch.Tensor) -> int:
@@ -158,7 +159,7 @@ def _device_problem(t: torch.Tensor) -> str | None:
     """Why `t` cannot be handed to the library as device memory, or None."""
     if not t.is_cuda:
         return "must be a device tensor"
-    if t.device.index != torch.cuda.current_device():
+    if t.get_device() != torch.cuda.current_device():
         return f"is on {t.device}, not on the current device"
     return None
 
@@ -580,14 +581,15 @@ def _row_sizes(rows: ExpertRows):
     """(N, E, k, R) of a set of rows, after checking them."""
     if not isinstance(rows, ExpertRows):
         raise ValueError("rows must be an ExpertRows (do_expert_rows)")
-    _want(rows.token_row, "rows.token_row", dtypes=_I32)
-    if rows.token_row.dim() != 2 or rows.offsets.dim() != 1:
+    offsets, row_token, token_row, token_expert = rows
+    _want(token_row, "rows.token_row", dtypes=_I32)
+    if not isinstance(offsets, torch.Tensor) or token_row.dim() != 2 or offsets.dim() != 1:
         raise ValueError("rows.token_row must have shape [N, k] and rows.offsets shape [E + 1]")
-    N, k = rows.token_row.shape
-    _want(rows.offsets, "rows.offsets", dtypes=_I32)
-    _want(rows.row_token, "rows.row_token", shape=(N * k,), dtypes=_I32)
-    _want(rows.token_expert, "rows.token_expert", shape=(N, k), dtypes=_I32)
-    return N, rows.offsets.shape[0] - 1, k, N * k
+    N, k = token_row.shape
+    _want(offsets, "rows.offsets", dtypes=_I32)
+    _want(row_token, "rows.row_token", shape=(N * k,), dtypes=_I32)
+    _want(token_expert, "rows.token_expert", shape=(N, k), dtypes=_I32)
+    return N, offsets.shape[0] - 1, k, N * k
 
 
 def _out(t: torch.Tensor | None, name: str, shape, dtype, device) -> torch.Tensor:
