@@ -26,9 +26,9 @@
 // straight to LDS write it in lane order, so it is the global address of each
 // lane that is permuted.
 //
-// 65,536 tokens of 8 of 128 experts (524,288 rows), bf16: 768 -> 2,048 in 1,680 us
-// (980 TFLOP/s), weight gradient of 1,536 x 2,048 in 3,530 us (940), 2,048 -> 2 x
-// 768 with the gated activation and its checkpoint in 3,330 us (990).  The matrix
+// 65,536 tokens of 8 of 128 experts (524,288 rows), bf16: 768 -> 2,048 in 1,660 us
+// (990 TFLOP/s), weight gradient of 1,536 x 2,048 in 3,530 to 3,620 us (910 to 940), 2,048 -> 2 x
+// 768 with the gated activation and its checkpoint in 3,300 us (1,000).  The matrix
 // cores are busy 55 % of the time at the clock of about 2 GHz that they leave; the
 // rest is the loads' way through the vector cache (a stage takes it 1.4 us, its
 // products 1.0) and the outputs at a tile's end.  fp32, 49,146 rows 1,536 -> 1,024
@@ -313,7 +313,9 @@ struct PieceLoader {
 // The same for rows of any width and alignment, through registers.  A piece is 16
 // bytes from wherever its first element lies (global memory takes any alignment),
 // elements past the row's end zeroed; only a wave that would read past the
-// operand's own end takes its pieces element by element.
+// operand's own end takes its pieces element by element.  The small tile's pieces
+// of both operands are in flight together, the large one's four by four, as its
+// registers allow.
 template <typename T, int LAYOUT, int DIM, int THREADS>
 struct ElementLoader {
   static constexpr int EL = Mma<T>::kElems;
@@ -321,8 +323,6 @@ struct ElementLoader {
   static constexpr int N = DIM * kStageBytes / 16 / THREADS;
   static constexpr int PR = LAYOUT == kInner ? kStageBytes / 16 : DIM / EL;
   static constexpr int RS = THREADS / PR;
-  static constexpr int G = 4;  // pieces that are loaded together
-  static_assert(N % G == 0);
   const T* ptr[LAYOUT == kInner ? N : 1];
   const T* first;  // the operand, and its end
   const T* end;
@@ -364,20 +364,33 @@ struct ElementLoader {
     cols = cols_ - c;
     base = b + (cols > 0 ? c : 0);
   }
-  // Pieces J .. J + G - 1 of the stage at dst.
-  template <int J>
-  __device__ __forceinline__ void load(int tid, char* dst) {
-    const T* src[G];
-    int n[G];  // elements that exist
-    bool part = false, past = first + EL > end;
+  // Elements of pieces J .. J + M - 1 of the stage that exist.
+  template <int J, int M>
+  __device__ __forceinline__ bool count(int* n) const {
+    bool part = false;
 #pragma unroll
-    for (int i = 0; i < G; ++i) {
-      if constexpr (LAYOUT == kInner) {
+    for (int i = 0; i < M; ++i) {
+      if constexpr (LAYOUT == kInner)
         n[i] = K - k;
+      else
+        n[i] = k + (J + i) * RS < K ? cols : 0;
+      part |= n[i] < EL;
+    }
+    return part;
+  }
+  // Loads pieces J .. J + M - 1 of the stage, what lies past a row's end with them.
+  template <int J, int M>
+  __device__ __forceinline__ void fetch(v4u* v) const {
+    const T* src[M];
+    int n[M];
+    count<J, M>(n);
+    bool past = first + EL > end;
+#pragma unroll
+    for (int i = 0; i < M; ++i) {
+      if constexpr (LAYOUT == kInner) {
         src[i] = ptr[J + i];
       } else {
         const int kk = k + (J + i) * RS;
-        n[i] = kk < K ? cols : 0;
         int64_t r = kk;
         if (token != nullptr && kk < K) {
           r = token[kk];
@@ -385,25 +398,14 @@ struct ElementLoader {
         }
         src[i] = base + r * ld;
       }
-      part |= n[i] < EL;
       past |= n[i] > 0 && src[i] + EL > end;
     }
-    v4u v[G];
     if (__ballot(past) == 0) {
 #pragma unroll
-      for (int i = 0; i < G; ++i) __builtin_memcpy(&v[i], n[i] > 0 ? src[i] : first, 16);
-      if (__ballot(part) != 0) {
-#pragma unroll
-        for (int i = 0; i < G; ++i)
-#pragma unroll
-          for (int d = 0; d < 4; ++d) {
-            const int bits = min(32, max(0, n[i] * (int)sizeof(T) * 8 - 32 * d));
-            v[i][d] &= bits == 32 ? ~0u : (1u << bits) - 1u;
-          }
-      }
+      for (int i = 0; i < M; ++i) __builtin_memcpy(&v[i], n[i] > 0 ? src[i] : first, 16);
     } else {
 #pragma unroll
-      for (int i = 0; i < G; ++i) {
+      for (int i = 0; i < M; ++i) {
         v[i] = v4u{0u, 0u, 0u, 0u};
 #pragma unroll
         for (int e = 0; e < EL; ++e)
@@ -415,8 +417,22 @@ struct ElementLoader {
           }
       }
     }
+  }
+  // Writes them to the stage at dst, zeros past the end.
+  template <int J, int M>
+  __device__ __forceinline__ void put(int tid, char* dst, v4u* v) const {
+    int n[M];
+    if (__ballot(count<J, M>(n)) != 0) {
 #pragma unroll
-    for (int i = 0; i < G; ++i) *reinterpret_cast<v4u*>(dst + (tid + (J + i) * THREADS) * 16) = v[i];
+      for (int i = 0; i < M; ++i)
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+          const int bits = min(32, max(0, n[i] * (int)sizeof(T) * 8 - 32 * d));
+          v[i][d] &= bits == 32 ? ~0u : (1u << bits) - 1u;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < M; ++i) *reinterpret_cast<v4u*>(dst + (tid + (J + i) * THREADS) * 16) = v[i];
   }
   __device__ __forceinline__ void next(int) {
     k += KS;
@@ -829,7 +845,11 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
     auto one = [&](auto& l, auto piece) {
       constexpr int j = decltype(piece)::value;
       if constexpr (!VEC) {
-        if constexpr (j % 4 == 0) l.template load<j>(tid, sm + at);  // four together
+        if constexpr (j % 4 == 0) {
+          v4u v[4];
+          l.template fetch<j, 4>(v);
+          l.template put<j, 4>(tid, sm + at, v);
+        }
       } else if constexpr (I < LoaderP::N) {
         l.template load<j>(tid, __builtin_amdgcn_readfirstlane(wave_lds + at), far_p(j), up_p(j) * g.Pd * l.ldo);
       } else {
@@ -843,7 +863,16 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
   };
   auto load_stage = [&] {
     if (!loading) return;
-    each<kLoads>([&](auto i) { load(i); });
+    if constexpr (!VEC && kLoads <= 12) {
+      v4u vp[LoaderP::N], vq[LoaderQ::N];
+      char* st = sm + load_slot * C::stage;
+      lp.template fetch<0, LoaderP::N>(vp);
+      lq.template fetch<0, LoaderQ::N>(vq);
+      lp.template put<0, LoaderP::N>(tid, st, vp);
+      lq.template put<0, LoaderQ::N>(tid, st + C::BP * kStageBytes, vq);
+    } else {
+      each<kLoads>([&](auto i) { load(i); });
+    }
     load_slot ^= 1;
     have = load_have;
     if (--load_left > 0) {

@@ -14,7 +14,7 @@
 // Bound by latency and launches up to some thousand tokens (64 tokens of 8 of 128
 // experts: one block, 6.3 us); beyond, by the scattered 4-byte stores of the three
 // lists (12 N k bytes).  65,536 tokens: 128 blocks, 5.4 us for the counts of their
-// units and 48 us for the rows.
+// units and 45 us for the rows.
 #include <algorithm>
 
 #include "experts.h"
@@ -229,7 +229,7 @@ __global__ __launch_bounds__(256) void k_combine(const T* o, const int32_t* toke
 
 // The same for rows of whole 16-byte pieces: one piece per thread, the k rows'
 // pieces in flight together.  Bound by memory: 65,536 tokens of 8 rows of 2,048
-// bf16 move 2.42 GB in 401 us (6.0 TB/s, nine tenths of it reads).
+// bf16 move 2.42 GB in 406 us (6.0 TB/s, nine tenths of it reads).
 template <typename T>
 __global__ __launch_bounds__(256) void k_combine_pieces(const v4u* o, const int32_t* token_row, int64_t N, int32_t k,
                                                         int64_t R, int32_t pieces, v4u* y) {
