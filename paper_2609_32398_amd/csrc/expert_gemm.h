@@ -129,14 +129,14 @@ __device__ __forceinline__ void wave_barrier() { asm volatile("s_waitcnt lgkmcnt
 
 // XOR pattern of a k-inner row's eight pieces: any eight or sixteen neighbouring
 // rows read at one piece touch different banks.
-__device__ __forceinline__ int inner_swizzle(int row) { return (row ^ (row >> 3 & 1)) & 7; }
+__host__ __device__ __forceinline__ int inner_swizzle(int row) { return (row ^ (row >> 3 & 1)) & 7; }
 
 // XOR pattern of the 16-byte pieces of k-outer rows, the same for all rows of a
 // thread: four neighbouring k of a transposed read (bf16) go to different banks.
 // fp32 operands are read 4 bytes a lane, two lanes to a bank, which its matrix
 // instructions hide.
 template <typename T, int DIM>
-__device__ __forceinline__ int outer_swizzle(int k) {
+__host__ __device__ __forceinline__ int outer_swizzle(int k) {
   return sizeof(T) == 2 ? (4 * (k & 3)) & (DIM * 2 / 16 - 1) : 0;
 }
 
@@ -145,6 +145,14 @@ __device__ __forceinline__ const char* uniform(const char* p) {
   const uint64_t v = reinterpret_cast<uint64_t>(p);
   const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
   return reinterpret_cast<const char*>(((uint64_t)hi << 32) | lo);
+}
+
+// Stages of a contraction of `have` (rows of an expert, or elements of a row).  None where there is nothing to
+// add up: an expert without rows may begin past the operands' last row, so not even its first row is there.
+template <typename T>
+__host__ __device__ __forceinline__ int stages(int have) {
+  constexpr int KS = kStageBytes / (int)sizeof(T);
+  return (have + KS - 1) / KS;
 }
 
 // The lane, as a value that is only known here: what is computed from it is not
@@ -197,8 +205,8 @@ struct PieceLoader {
   int32_t pos, K;      // first k of the stage
   int32_t turn = 0;    // the list in use
 
-  static __device__ __forceinline__ int row(int tid) { return tid / PR; }
-  static __device__ __forceinline__ int piece(int tid) {
+  static __host__ __device__ __forceinline__ int row(int tid) { return tid / PR; }
+  static __host__ __device__ __forceinline__ int piece(int tid) {
     const int slot = tid % PR;
     if constexpr (LAYOUT == kInner)
       return slot ^ inner_swizzle(row(tid));
@@ -206,7 +214,7 @@ struct PieceLoader {
       return slot ^ outer_swizzle<T, DIM>(row(tid));
   }
   // the first k of a thread's piece in its stage
-  static __device__ __forceinline__ int first_k(int tid, int j) {
+  static __host__ __device__ __forceinline__ int first_k(int tid, int j) {
     return LAYOUT == kInner ? piece(tid) * EL : row(tid) + j * RS;
   }
   // k inner, rows by token: rowi(j) is the operand row of the thread's j-th piece
@@ -219,7 +227,7 @@ struct PieceLoader {
     shorten(tid);
   }
   // k inner: rows b + (row0 + i) * ld, not past row `end`
-  __device__ __forceinline__ void start_inner(int tid, int32_t K_, const T* b, int32_t ld, int32_t row0, int32_t end) {
+  __host__ __device__ __forceinline__ void start_inner(int tid, int32_t K_, const T* b, int32_t ld, int32_t row0, int32_t end) {
     begin(K_, b, ld);
     step = kStageBytes;
     off[0] = (uint32_t)(row0 + row(tid)) * ldo + piece(tid) * EL / kUnit * kBytes;
@@ -227,7 +235,7 @@ struct PieceLoader {
     shorten(tid);
   }
   // k outer: rows b + k * ld (or b + tok[k] * ld), columns col0 .. of `cols`
-  __device__ __forceinline__ void start_outer(int tid, int32_t K_, const T* b, int32_t ld, int32_t col0, int32_t cols,
+  __host__ __device__ __forceinline__ void start_outer(int tid, int32_t K_, const T* b, int32_t ld, int32_t col0, int32_t cols,
                                               const int32_t* tok, int64_t last_, const int32_t* lists) {
     begin(K_, b, ld);
     const int c = col0 + piece(tid) * EL;
@@ -245,13 +253,13 @@ struct PieceLoader {
       off[0] = (uint32_t)row(tid) * ldo + lim;
     }
   }
-  __device__ __forceinline__ void begin(int32_t K_, const T* b, int32_t ld) {
+  __host__ __device__ __forceinline__ void begin(int32_t K_, const T* b, int32_t ld) {
     base = reinterpret_cast<const char*>(b);
     left = K = K_;
     ldo = (uint32_t)ld / kUnit * kBytes;
   }
   // A short stage, k inner: pieces past the end take the place of the first k.
-  __device__ __forceinline__ void shorten(int tid) {
+  __host__ __device__ __forceinline__ void shorten(int tid) {
     if constexpr (LAYOUT == kInner) {
       if (left < KS && first_k(tid, 0) >= left) {
         const uint32_t back = (uint32_t)first_k(tid, 0) / kUnit * kBytes;
@@ -271,10 +279,10 @@ struct PieceLoader {
       word_to_lds(token + max(0, min(pos + tid + i * THREADS, K - 1)),
                   __builtin_amdgcn_readfirstlane(dst + i * THREADS * 4));
   }
-  // Piece J of the stage to LDS byte address dst (uniform: the wave's place in the operand's stage).
+  // The offset of piece J of the stage.
   // far: where the rows of piece J lie from those of piece 0 (k inner).
   template <int J>
-  __device__ __forceinline__ void load(int tid, uint32_t dst, uint32_t far, uint32_t up) {
+  __host__ __device__ __forceinline__ uint32_t offset(int tid, uint32_t far, uint32_t up) const {
     uint32_t o;
     if constexpr (LAYOUT == kOuter) {
       if constexpr (GATHER) {  // an index below 0 is clamped to the last row
@@ -286,14 +294,21 @@ struct PieceLoader {
     } else if constexpr (GATHER) {
       o = off[J];
     } else {
-      o = min(off[0] + far * ldo, lim) + up;
+      o = off[0] + far * ldo;
+      o = (o < lim ? o : lim) + up;
     }
+    return o;
+  }
+  // Piece J of the stage to LDS byte address dst (uniform: the wave's place in the operand's stage).
+  template <int J>
+  __device__ __forceinline__ void load(int tid, uint32_t dst, uint32_t far, uint32_t up) {
+    const uint32_t o = offset<J>(tid, far, up);
     if constexpr (WIDE)
       load_to_lds<J * THREADS * 16>(base + (uint64_t)o * 16, dst);
     else
       load_to_lds<J * THREADS * 16>(uniform(base), o, dst);
   }
-  __device__ __forceinline__ void next(int tid) {
+  __host__ __device__ __forceinline__ void next(int tid) {
     if constexpr (LAYOUT == kOuter && GATHER) {
       pos += KS;
       if ((pos & (kList - 1)) == 0) fetch(tid);
@@ -755,7 +770,8 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
       w.rows = __builtin_amdgcn_readfirstlane(min(C::BQ, n - i / PT * C::BQ));
       w.have = g.K;
     }
-    w.nk = max(1, (w.have + KS - 1) / KS);
+    w.nk = stages<T>(w.have);
+    if constexpr (EPI != kWeightGrad) w.nk = max(1, w.nk);  // K is 1 at least: a loop with its test at the end
     return w;
   };
   if constexpr (!VEC) {
@@ -792,10 +808,8 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
     const T* P = static_cast<const T*>(g.P);
     const T* Q = static_cast<const T*>(g.Q);
     if constexpr (EPI == kWeightGrad) {
-      // an expert without rows may begin at the lists' end, where there is no token to look at
-      const int32_t t0 = (int32_t)min((int64_t)w.r0, g.R - 1);
-      const int32_t* pt = GP ? g.p_token + t0 : nullptr;
-      const int32_t* qt = GQ ? g.q_token + t0 : nullptr;
+      const int32_t* pt = GP ? g.p_token + w.r0 : nullptr;
+      const int32_t* qt = GQ ? g.q_token + w.r0 : nullptr;
       lp.start_outer(tid, w.rows, pt ? P : P + (int64_t)w.r0 * g.ldp, g.ldp, w.p0, g.Pd, pt, g.N - 1, lists);
       lq.start_outer(tid, w.rows, qt ? Q : Q + (int64_t)w.r0 * g.ldq, g.ldq, w.q0, g.Qd, qt, g.N - 1, lists + (GP ? 2 * kList : 0));
     } else {
@@ -825,17 +839,29 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
 
   // The loaders run a stage ahead of the products, through the tiles in the same order.
   const bool loader = tid < C::loaders;
-  Where wl = locate(tile);
-  int load_tile = tile, load_left = wl.nk, load_slot = 0;
-  int32_t load_have = wl.have, have = wl.have;  // k from the next stage's first on, and from the last loaded one's
-  bool loading = true;
+  int load_tile = tile;  // the first one to load
+  Where wl;
   Tokens kn;
-  if (loader) {
-    start(wl, tokens(wl));
-    if (load_tile + tile_step < tile_end) {
-      wl = locate(load_tile + tile_step);
+  // wl: the first tile from t on that has something to load, if there is one (an expert without rows has no
+  // stage, though its gradient's tiles are written)
+  auto look = [&](int t) {
+    if constexpr (EPI == kWeightGrad) {
+      while (t < tile_end && (wl = locate(t)).nk == 0) t += tile_step;
+    } else if (t < tile_end) {
+      wl = locate(t);
       kn = tokens(wl);
     }
+    return t;
+  };
+  wl = locate(tile);
+  if constexpr (EPI == kWeightGrad) load_tile = look(tile);
+  bool loading = load_tile < tile_end;
+  int load_left = wl.nk, load_slot = 0;
+  int32_t load_have = wl.have, have = wl.have;  // k from the next stage's first on, and from the last loaded one's
+  int next_tile = tile_end;
+  if (loader && loading) {
+    start(wl, tokens(wl));
+    next_tile = look(load_tile + tile_step);
   }
   // piece I of a thread's pieces of the next stage, P's then Q's
   constexpr int kLoads = LoaderP::N + LoaderQ::N;
@@ -880,16 +906,12 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
       lq.next(tid);
       load_have -= KS;
     } else {
-      load_tile += tile_step;
-      loading = load_tile < tile_end;
+      loading = next_tile < tile_end;
       if (loading) {
         start(wl, kn);
         load_left = wl.nk;
         load_have = wl.have;
-        if (load_tile + tile_step < tile_end) {
-          wl = locate(load_tile + tile_step);
-          kn = tokens(wl);
-        }
+        next_tile = look(next_tile + tile_step);
       }
     }
   };
@@ -928,6 +950,9 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
   int buf = 0;
   for (; tile < tile_end; tile += tile_step) {
     const Where w = locate(tile);
+    if constexpr (EPI == kWeightGrad) {
+      if (w.nk == 0 && g.accumulate) continue;  // nothing to add
+    }
     v16f acc[C::MP][C::MQ];
 #pragma unroll
     for (int i = 0; i < C::MP; ++i)
