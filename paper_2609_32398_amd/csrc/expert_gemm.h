@@ -147,6 +147,9 @@ __device__ __forceinline__ const char* uniform(const char* p) {
   return reinterpret_cast<const char*>(((uint64_t)hi << 32) | lo);
 }
 
+// Token t of those up to `last`: an index out of range counts as the nearest one in it.
+__host__ __device__ __forceinline__ int32_t clip_token(int32_t t, int32_t last) { return max(0, min(t, last)); }
+
 // Stages of a contraction of `have` (rows of an expert, or elements of a row).  None where there is nothing to
 // add up: an expert without rows may begin past the operands' last row, so not even its first row is there.
 template <typename T>
@@ -199,7 +202,7 @@ struct PieceLoader {
   uint32_t off[LAYOUT == kInner && GATHER ? N : 1], lim;
   // k outer, by token: the tokens come through LDS, kList of them at a time in two lists
   const int32_t* token;
-  uint32_t last;       // last row of the gathered operand
+  int32_t last;        // last row of the gathered operand
   const int32_t* list;
   uint32_t list_lds;   // its LDS byte address
   int32_t pos, K;      // first k of the stage
@@ -243,7 +246,7 @@ struct PieceLoader {
     if constexpr (GATHER) {
       step = 0;
       token = tok;
-      last = (uint32_t)last_;
+      last = (int32_t)last_;
       pos = 0;
       list = lists;
       list_lds = (uint32_t)(uintptr_t)(const DOL_LDS char*)(lists);
@@ -285,8 +288,8 @@ struct PieceLoader {
   __host__ __device__ __forceinline__ uint32_t offset(int tid, uint32_t far, uint32_t up) const {
     uint32_t o;
     if constexpr (LAYOUT == kOuter) {
-      if constexpr (GATHER) {  // an index below 0 is clamped to the last row
-        o = min((uint32_t)list[turn * kList + (pos & (kList - 1)) + row(tid) + J * RS], last) * ldo + lim;
+      if constexpr (GATHER) {
+        o = (uint32_t)clip_token(list[turn * kList + (pos & (kList - 1)) + row(tid) + J * RS], last) * ldo + lim;
       } else {
         o = off[0] + J * RS * ldo;
         if (left < KS) o = first_k(tid, J) < left ? o : lim;
@@ -408,8 +411,7 @@ struct ElementLoader {
         const int kk = k + (J + i) * RS;
         int64_t r = kk;
         if (token != nullptr && kk < K) {
-          r = token[kk];
-          r = r < 0 || r > last ? last : r;
+          r = clip_token(token[kk], (int32_t)last);
         }
         src[i] = base + r * ld;
       }
@@ -675,9 +677,7 @@ __device__ __forceinline__ float prob_at(const ExpertGemm& g, int64_t i) {
 // The routing probability of row r of expert e (1 without probabilities).
 __device__ __forceinline__ float row_prob(const ExpertGemm& g, int64_t r, int e) {
   if (g.prob == nullptr) return 1.0f;
-  int64_t t = g.q_token[r];
-  t = t < 0 ? 0 : (t >= g.N ? g.N - 1 : t);
-  return prob_at(g, t * g.E + e);
+  return prob_at(g, (int64_t)clip_token(g.q_token[r], (int32_t)(g.N - 1)) * g.E + e);
 }
 
 // LDS beside the stages: lists of tokens (k outer only) and probabilities of a tile's rows.
@@ -825,8 +825,8 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
         lp.start_outer(tid, g.K, P + (int64_t)w.e * g.K * g.ldp, g.ldp, w.p0, g.Pd, nullptr, 0, nullptr);
       }
       if constexpr (GQ) {
-        const uint32_t last = (uint32_t)g.N - 1u;
-        lq.start_rows(tid, g.K, Q, g.ldq, [&](int j) { return min((uint32_t)k.t[j], last); });
+        const int32_t last = (int32_t)(g.N - 1);
+        lq.start_rows(tid, g.K, Q, g.ldq, [&](int j) { return clip_token(k.t[j], last); });
       } else if constexpr (VEC) {
         lq.start_inner(tid, g.K, Q + (int64_t)w.r0 * g.ldq, g.ldq, 0, w.rows - 1);
       } else {

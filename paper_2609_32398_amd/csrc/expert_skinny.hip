@@ -80,8 +80,7 @@ __global__ __launch_bounds__(kWaves* kWave) void k_expert_skinny(const ExpertGem
   const int row = lane & 15, at = (lane >> 4) * EL;
   int64_t xr = r0 + min(row, rows - 1);
   if constexpr (GQ) {
-    xr = g.q_token[xr];
-    xr = xr < 0 ? 0 : (xr >= g.N ? g.N - 1 : xr);
+    xr = clip_token(g.q_token[xr], (int32_t)(g.N - 1));
   }
   const T* x = static_cast<const T*>(g.Q) + xr * g.ldq;
   const T* we = static_cast<const T*>(g.P) + (int64_t)e * (EPI == kSwiglu ? 2 * g.Pd : g.Pd) * g.ldp;
