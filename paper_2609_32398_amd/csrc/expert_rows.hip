@@ -16,6 +16,7 @@
 // lists (12 N k bytes).  65,536 tokens: 128 blocks, 5.4 us for the counts of their
 // units and 45 us for the rows.
 #include <algorithm>
+#include <atomic>
 
 #include "experts.h"
 
@@ -295,6 +296,21 @@ __global__ __launch_bounds__(256) void k_expert_dp(const float* part, int32_t pa
   for (int i = threadIdx.x; i < n * E; i += 256) dp[t0 * E + i] = from_float<T>(rows[i]);
 }
 
+// The kernels' LDS limits, for any E and once per device: a limit set for one call could be too small for
+// another thread's.
+hipError_t allow_lds() {
+  static std::atomic<bool> done[64];
+  const int device = device_info().device;
+  if (device < 0 || device >= 64) return hipErrorInvalidDevice;
+  if (done[device].load(std::memory_order_acquire)) return hipSuccess;
+  for (const void* kern : {reinterpret_cast<const void*>(k_row_counts), reinterpret_cast<const void*>(k_rows)}) {
+    const hipError_t e = hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, kMaxE * (64 + 4));
+    if (e != hipSuccess) return e;
+  }
+  done[device].store(true, std::memory_order_release);
+  return hipSuccess;
+}
+
 }  // namespace
 
 hipError_t launch_expert_rows(const u64* bits, int64_t N, int32_t E, int32_t k, int32_t* offsets, int32_t* row_token,
@@ -302,14 +318,9 @@ hipError_t launch_expert_rows(const u64* bits, int64_t N, int32_t E, int32_t k, 
   const int64_t U = (N + 511) / 512;
   const int64_t chunks = std::min<int64_t>(U, kRowChunks);
   const size_t masks = (size_t)E * 64, lds = masks + (size_t)E * 4;
-  hipError_t e;
-  if ((e = hipFuncSetAttribute(reinterpret_cast<const void*>(k_rows), hipFuncAttributeMaxDynamicSharedMemorySize,
-                               (int)lds)) != hipSuccess)
-    return e;
+  hipError_t e = allow_lds();
+  if (e != hipSuccess) return e;
   if (U > 1) {
-    if ((e = hipFuncSetAttribute(reinterpret_cast<const void*>(k_row_counts),
-                                 hipFuncAttributeMaxDynamicSharedMemorySize, (int)masks)) != hipSuccess)
-      return e;
     hipLaunchKernelGGL(k_row_counts, dim3((unsigned)chunks), dim3(kRowThreads), masks, s, bits, N, E, k, counts);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }

@@ -1,0 +1,67 @@
+"""What the experts' entry points ask of HIP, recorded on the host in place of a GPU."""
+import json
+import os
+import subprocess
+import sys
+
+import pytest
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+
+# Run in a process of its own: the stand-ins are found before the HIP library's functions.
+RUN = r"""
+import ctypes, json, sys
+
+class Record(ctypes.Structure):
+    _fields_ = [("func", ctypes.c_void_p), ("limit", ctypes.c_int64), ("shared", ctypes.c_int64),
+                ("blocks", ctypes.c_int64), ("threads", ctypes.c_int64)]
+
+hip = ctypes.CDLL(sys.argv[1], mode=ctypes.RTLD_GLOBAL)
+lib = ctypes.CDLL(sys.argv[2])
+i64, i32, vp = ctypes.c_int64, ctypes.c_int32, ctypes.c_void_p
+FAKE = 0x10000
+for name, types, args in json.loads(sys.argv[3]):
+    f = getattr(lib, name)
+    f.argtypes, f.restype = [{"l": i64, "i": i32, "p": vp}[t] for t in types], i32
+    status = f(*[FAKE if a == "p" else a for a in args])
+    assert status == 0, (name, args, status)
+records = (Record * 4096).in_dll(hip, "records")
+print(json.dumps([[r.func, r.limit, r.shared, r.blocks, r.threads]
+                  for r in records[:ctypes.c_int.in_dll(hip, "n_records").value]]))
+"""
+
+
+@pytest.fixture(scope="module")
+def record(tmp_path_factory):
+    import paper_2609_32398_amd as p
+
+    if not os.path.exists(p.LIB_PATH):
+        p.build()
+    so = str(tmp_path_factory.mktemp("hip") / "libhip_recorder.so")
+    subprocess.run(["gcc", "-O1", "-shared", "-fPIC", os.path.join(HERE, "hip_recorder.c"), "-o", so], check=True)
+
+    def run(calls):
+        r = subprocess.run([sys.executable, "-c", RUN, so, p.LIB_PATH, json.dumps(calls)], capture_output=True,
+                           text=True, timeout=100)
+        assert r.returncode == 0, r.stderr[-2000:]
+        return json.loads(r.stdout)
+
+    return run
+
+
+def _rows(N, E, k):
+    return ["do_expert_rows", "pliippppplp", ["p", N, E, k, "p", "p", "p", "p", "p", 1 << 40, None]]
+
+
+def test_rows_of_many_and_of_few_experts_share_one_limit(record):
+    # Another thread may launch between a call's limit and its launch: a call must not lower it.
+    got = record([_rows(600, 1024, 8), _rows(600, 8, 2), _rows(100, 512, 2), _rows(5000, 1024, 1)])
+    limits, launches = {}, 0
+    for func, limit, shared, blocks, threads in got:
+        if limit >= 0:
+            assert limit >= limits.get(func, 0), "a call lowers the limit that another one's launch needs"
+            limits[func] = limit
+        else:
+            assert shared <= limits[func]
+            launches += 1
+    assert launches == 2 + 2 + 1 + 2  # counts and rows; one unit: the rows alone
