@@ -26,12 +26,13 @@ import paper_2609_32398_amd as dl  # noqa: E402
 
 
 class _Experts(torch.autograd.Function):
-    """(y, surrogate loss) of tokens x [N, H], probabilities p [N, E] and router scores [N, E]."""
+    """(y, surrogate loss) of tokens x [N, H], probabilities p [N, E] and router scores [N, E].  training: keep
+    what the backward pass reads (within a Function one cannot tell: the inputs say whether they require
+    gradients, not whether any are recorded)."""
 
     @staticmethod
-    def forward(ctx, x, p, scores, w1, w2, k):
+    def forward(ctx, x, p, scores, w1, w2, k, training):
         N = x.shape[0]
-        training = any(ctx.needs_input_grad)
         bits, D, _ = dl.do_fused(scores[None], k, want_bits=True)
         rows = dl.do_expert_rows(bits, N, k)
         h, kept = dl.do_expert_swiglu(x, w1, rows, p, checkpoint=training)
@@ -50,7 +51,7 @@ class _Experts(torch.autograd.Function):
         dw2 = dl.do_expert_weight_grad(dy, h, rows, gather_dy=True)
         dw1 = dl.do_expert_weight_grad(da, x, rows, gather_x=True)
         dx = dl.do_expert_combine(dl.do_expert_matmul(da, w1, rows, transposed=True), rows)
-        return dx, dp + (dl_do * dloss).to(dp.dtype), None, dw1.to(w1.dtype), dw2.to(w2.dtype), None
+        return dx, dp + (dl_do * dloss).to(dp.dtype), None, dw1.to(w1.dtype), dw2.to(w2.dtype), None, None
 
 
 class MoELayer(torch.nn.Module):
@@ -73,7 +74,8 @@ class MoELayer(torch.nn.Module):
         """y [N, H] and the surrogate loss of x [N, H]."""
         scores = torch.nn.functional.linear(x, self.router).float()
         p = torch.softmax(scores, dim=1)
-        return _Experts.apply(x.contiguous(), p, scores.detach(), self.w1, self.w2, self.k)
+        training = torch.is_grad_enabled() and any(t.requires_grad for t in (x, p, self.w1, self.w2))
+        return _Experts.apply(x.contiguous(), p, scores.detach(), self.w1, self.w2, self.k, training)
 
 
 def train(steps=40, tokens=4096, H=256, F=256, E=16, k=2, dtype=torch.bfloat16, weight=0.0, seed=0, log=print):
