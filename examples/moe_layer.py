@@ -39,15 +39,14 @@ class _Experts(torch.autograd.Function):
         y = dl.do_expert_combine(dl.do_expert_matmul(h, w2, rows), rows)
         loss, dloss = dl.do_surrogate(p[None], k, bits, D, want_grad=training)
         if training:
-            ctx.rows, ctx.kept = rows, kept
-            ctx.save_for_backward(x, p, w1, w2, dloss[0])
+            ctx.save_for_backward(x, p, w1, w2, dloss[0], *rows, *kept)
         return y, loss[0].float()
 
     @staticmethod
     def backward(ctx, dy, dl_do):
-        x, p, w1, w2, dloss = ctx.saved_tensors
-        rows, dy = ctx.rows, dy.contiguous()
-        da, h, dp = dl.do_expert_swiglu_grad(dy, w2, rows, ctx.kept, p)
+        x, p, w1, w2, dloss, *rest = ctx.saved_tensors
+        rows, kept, dy = dl.ExpertRows(*rest[:-2]), dl.Act8(*rest[-2:]), dy.contiguous()
+        da, h, dp = dl.do_expert_swiglu_grad(dy, w2, rows, kept, p)
         dw2 = dl.do_expert_weight_grad(dy, h, rows, gather_dy=True)
         dw1 = dl.do_expert_weight_grad(da, x, rows, gather_x=True)
         dx = dl.do_expert_combine(dl.do_expert_matmul(da, w1, rows, transposed=True), rows)

@@ -80,3 +80,12 @@ def test_training_keeps_the_checkpoint(layer_and_calls):
     assert calls.kept == {"checkpoint": True, "gradient": True}
     (y.sum() + loss).backward()
     assert all(q.grad is not None for q in layer.parameters())
+
+
+def test_what_is_kept_goes_through_saved_tensors(layer_and_calls):
+    # so that hooks (to offload, to count) see the 8-bit values too
+    layer, _ = layer_and_calls
+    seen = []
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: seen.append(t.dtype) or t, lambda t: t):
+        layer(torch.randn(N, H))
+    assert torch.int8 in seen and torch.uint8 in seen
