@@ -44,6 +44,8 @@ class _Experts(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, dy, dl_do):
+        if torch.is_grad_enabled():  # create_graph: the gradients' own derivatives would be left out silently
+            raise RuntimeError("the experts' operators have no second derivative")
         x, p, w1, w2, dloss, *rest = ctx.saved_tensors
         rows, kept, dy = dl.ExpertRows(*rest[:-2]), dl.Act8(*rest[-2:]), dy.contiguous()
         da, h, dp = dl.do_expert_swiglu_grad(dy, w2, rows, kept, p)

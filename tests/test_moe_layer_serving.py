@@ -89,3 +89,12 @@ def test_what_is_kept_goes_through_saved_tensors(layer_and_calls):
     with torch.autograd.graph.saved_tensors_hooks(lambda t: seen.append(t.dtype) or t, lambda t: t):
         layer(torch.randn(N, H))
     assert torch.int8 in seen and torch.uint8 in seen
+
+
+def test_a_second_derivative_is_refused(layer_and_calls):
+    layer, _ = layer_and_calls
+    x = torch.randn(N, H, requires_grad=True)
+    y, _ = layer(x)
+    with pytest.raises(RuntimeError):
+        (g,) = torch.autograd.grad(y.sum(), x, create_graph=True)
+        g.sum().backward()
