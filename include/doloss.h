@@ -372,10 +372,10 @@ do_status do_rem_dispatch(const do_rem_move* replicas, const int32_t* n_replicas
  * on the device: no call waits.
  *   Rows past offsets[E] are neither read nor written.  Token indices are
  *   clamped to [0, N), offsets to [0, R].
- *   Limits: 1 <= E <= 1024, N and R in [1, 2^31), widths in [1, 65536]
- *   (DO_ERR_OVERFLOW where a tile list would pass 2^31).  Any width and
- *   element alignment is accepted; rows of whole 16-byte pieces at 16-byte
- *   aligned addresses take the fast path.
+ *   Limits: 1 <= E <= 1024, N in [1, 2^31), R in [1, 2^31 - 1024], widths in
+ *   [1, 65536] (DO_ERR_OVERFLOW past N's and R's, or where a tile list would
+ *   pass 2^31).  Any width and element alignment is accepted; rows of whole
+ *   16-byte pieces at 16-byte aligned addresses take the fast path.
  */
 
 /*

@@ -40,11 +40,12 @@ do_status check_experts(int64_t N, int32_t E, int32_t k) {
     return set_error(DO_ERR_OVERFLOW, "N * k must be < 2^31 (rows are int32)");
   return DO_OK;
 }
-do_status check_rows(int64_t N, int64_t R, int32_t E) {
+// most: rows of the products (dol::kMaxRows), or whatever int32 holds.
+do_status check_rows(int64_t N, int64_t R, int32_t E, int64_t most = dol::kMaxRows) {
   if (E < 1 || E > dol::kMaxE) return set_error(DO_ERR_INVALID_ARG, "E must be in [1, 1024]");
   if (N < 1 || R < 1) return set_error(DO_ERR_INVALID_ARG, "N and R must be >= 1");
-  if (N >= (int64_t(1) << 31) || R >= (int64_t(1) << 31))
-    return set_error(DO_ERR_OVERFLOW, "N and R must be < 2^31 (rows are int32)");
+  if (N >= (int64_t(1) << 31) || R > most)
+    return set_error(DO_ERR_OVERFLOW, "N must be < 2^31 and R at most 2^31 - 1024 (rows are int32)");
   return DO_OK;
 }
 do_status check_widths(int64_t R, int32_t E, std::initializer_list<int32_t> w) {
@@ -309,7 +310,7 @@ DOLOSS_API do_status do_expert_swiglu_grad(const void* dy, const void* w2, do_dt
 DOLOSS_API do_status do_act8_pack(const void* x, do_dtype dtype, int64_t rows, int32_t W, int8_t* q, uint8_t* e,
                                   hipStream_t stream) {
   DO_TRY(check_dtype(dtype));
-  DO_TRY(check_rows(1, rows, 1));
+  DO_TRY(check_rows(1, rows, 1, (int64_t(1) << 31) - 1));
   DO_TRY(check_widths(1, 1, {W}));
   DO_TRY(check_ptr(x, size_of(dtype), "x is NULL or not aligned to its element size"));
   DO_TRY(check_ptr(q, 1, "q is NULL"));
@@ -320,7 +321,7 @@ DOLOSS_API do_status do_act8_pack(const void* x, do_dtype dtype, int64_t rows, i
 DOLOSS_API do_status do_act8_unpack(const int8_t* q, const uint8_t* e, int64_t rows, int32_t W, void* x,
                                     do_dtype dtype, hipStream_t stream) {
   DO_TRY(check_dtype(dtype));
-  DO_TRY(check_rows(1, rows, 1));
+  DO_TRY(check_rows(1, rows, 1, (int64_t(1) << 31) - 1));
   DO_TRY(check_widths(1, 1, {W}));
   DO_TRY(check_ptr(q, 1, "q is NULL"));
   DO_TRY(check_ptr(e, 1, "e is NULL"));

@@ -9,6 +9,8 @@ namespace dol {
 
 constexpr int kAct8Group = 32;          // elements that share one exponent byte
 constexpr int32_t kMaxWidth = 1 << 16;  // of a row of activations or weights
+// Rows of a product: a tile's rows, a stage and a list of 1,024 tokens are added to a row's number in int32.
+constexpr int64_t kMaxRows = (int64_t(1) << 31) - 1024;
 
 // do_last_error of the calling thread, and the status itself.
 do_status set_error(do_status st, const char* msg);
