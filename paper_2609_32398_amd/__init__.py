@@ -765,7 +765,7 @@ def do_act8_pack(x: torch.Tensor) -> Act8:
 
 def do_act8_unpack(a: Act8, dtype: torch.dtype, out: torch.Tensor | None = None) -> torch.Tensor:
     """The values of an Act8 in float32 or bfloat16."""
-    if not isinstance(a, Act8) or a.q.dim() < 1 or a.q.numel() == 0:
+    if not isinstance(a, Act8) or not isinstance(a.q, torch.Tensor) or a.q.dim() < 1 or a.q.numel() == 0:
         raise ValueError("a must be an Act8 with at least one element")
     if dtype not in _SCORE_DTYPES:
         raise ValueError(f"dtype {dtype} is not one of {_SCORE_DTYPES}")

@@ -82,3 +82,13 @@ def test_rows_whose_sums_pass_int32_are_refused(record):
 
     record(calls(most))
     assert record(calls(most + 2), expect=[4, 4, 4, 4]) == []  # refused, and nothing launched
+
+
+def test_an_act8_of_no_tensors_is_refused():
+    import torch
+
+    import paper_2609_32398_amd as dl
+
+    for a in (dl.Act8(None, None), dl.Act8(3, 4), dl.Act8([1], [2])):
+        with pytest.raises(ValueError):
+            dl.do_act8_unpack(a, torch.float32)
