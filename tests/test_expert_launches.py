@@ -92,3 +92,40 @@ def test_an_act8_of_no_tensors_is_refused():
     for a in (dl.Act8(None, None), dl.Act8(3, 4), dl.Act8([1], [2])):
         with pytest.raises(ValueError):
             dl.do_act8_unpack(a, torch.float32)
+
+
+def _matmul(N, R, E, O, I, dtype, transposed=0):
+    return ["do_expert_matmul", "ppipplliiiipp", ["p", "p", dtype, "p", "p", N, R, E, O, I, transposed, "p", None]]
+
+
+def _swiglu(N, R, E, H, F, dtype):
+    return ["do_expert_swiglu", "ppipipplliiipppp", ["p", "p", dtype, "p", 0, "p", "p", N, R, E, H, F, "p", "p", "p", None]]
+
+
+def _wgrad(N, R, E, O, I, dtype, dy_token=None, x_token=None):
+    return ["do_expert_weight_grad", "ppippplliiiipp", ["p", "p", dtype, "p", dy_token, x_token, N, R, E, O, I, 0, "p", None]]
+
+
+def _threads(record, call):
+    launches = [r for r in record([call]) if r[1] < 0]
+    assert len(launches) == 1
+    return launches[0][4], launches[0][3], launches[0][2]
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_the_gpu_tests_shapes_reach_their_tiles(record, dtype):
+    import test_gpu_expert_tiles as t
+
+    for N, E, k, O, I in t.FEW:
+        assert _threads(record, _matmul(N, N * k, E, O, I, dtype))[0] == 128
+        assert _threads(record, _matmul(N, N * k, E, I, O, dtype, 1))[0] == (128 if O * (4 >> dtype) % 16 == 0 and I * (4 >> dtype) % 16 == 0 else 256)
+    for N, E, k, H, F in t.FEW_GATED:
+        assert _threads(record, _swiglu(N, N * k, E, H, F, dtype))[0] == 128
+    # the kernel of few rows: four waves and no dynamic shared memory
+    for N, E, k, O, I in t.SKINNY:
+        assert _threads(record, _matmul(N, N * k, E, O, I, dtype))[::2] == (256, 0)
+    for N, E, k, H, F in t.SKINNY_GATED:
+        assert _threads(record, _swiglu(N, N * k, E, H, F, dtype))[::2] == (256, 0)
+    for E, O, I in t.LARGE:
+        for dy, x in ((None, None), ("p", None), (None, "p"), ("p", "p")):
+            assert _threads(record, _wgrad(2600, 5200, E, O, I, dtype, dy, x))[0] == 512
