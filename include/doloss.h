@@ -368,10 +368,11 @@ do_status do_rem_dispatch(const do_rem_move* replicas, const int32_t* n_replicas
  * expert layer y_t = sum_e p_te W2_e (silu(g) u), (g, u) = W1_e x_t, and its
  * gradients, row by row.  `dtype` is the type of activations and weights
  * (DO_F32 or DO_BF16); products, sums and activations are computed in fp32 and
- * rounded once (to nearest even) where they are stored.  Row counts are read
- * on the device: no call waits.
- *   Rows past offsets[E] are neither read nor written.  Token indices are
- *   clamped to [0, N), offsets to [0, R].
+ * rounded once (to nearest even) where they are stored; 1 / (1 + e^-g) is off
+ * by about |g| + 2 units in fp32's last place.  Row counts are read on the
+ * device: no call waits.
+ *   Rows past offsets[E] are neither used nor written.  Token indices are
+ *   clamped to [0, N), offsets to [0, R].  Outputs overlap no input.
  *   Limits: 1 <= E <= 1024, N in [1, 2^31), R in [1, 2^31 - 1024], widths in
  *   [1, 65536] (DO_ERR_OVERFLOW past N's and R's, or where a tile list would
  *   pass 2^31).  Any width and element alignment is accepted; rows of whole

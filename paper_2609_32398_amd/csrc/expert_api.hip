@@ -71,12 +71,16 @@ bool whole_expert(const void* w, do_dtype dt, int32_t row, int64_t rows) {
 }
 
 // Whether there are few rows, and the experts that can have them are so few that their tiles of `cols`
-// weight rows leave CUs idle, or, in fp32, whose matrix instructions take 16 times as long, fill them less than twice: then a
-// tile's time counts, and it is shorter with a quarter of the contraction for each wave.  Against the
-// tiles that share LDS, 8 experts a token, 768 -> 2,048 and gated 2,048 -> 2 x 768: bf16, 1 token 16.7 and
-// 19.4 us against 16.7 and 24.7 (within the rule), 4 tokens 26.0 and 44.4 against 17.7 and 41.0 (outside);
-// fp32, 1 token 17.6 and 32.6 against 34.2 and 84.8, 4 tokens 43.1 and 79.3 against 56.9 and 142.9
-// (within), 16 tokens 90.1 and 158 against 89.8 and 149 (outside).
+// weight rows leave CUs idle, or, in fp32, whose matrix instructions take 16 times as long, fill them less
+// than twice: then a tile's time counts, and it is shorter with a quarter of the contraction for each wave.
+// Against the tiles that share LDS, 8 of 128 experts a token, 768 -> 2,048 and gated 2,048 -> 2 x 768, calls in
+// a graph whose weights come from memory: bf16, 1 token 10.2 and 18.4 us against 13.8 and 31.8, 2 tokens (at the
+// rule's edge) 16.3 and 29.9 against 15.8 and 34.7, 4 tokens (outside) 26.0 and 43.7 against 19.3 and 40.0;
+// fp32, 1 token 18.7 and 35.1 against 34.4 and 83.7, 4 tokens (the edge) 49.6 and 84.0 against 57.4 and 139,
+// 16 tokens (outside) 123 and 222 against 114 and 227.  Few experts keep within the rule up to 16 rows each on
+// average, where some then have two tiles of 16 rows: 2 of 8 experts, 1,536 -> 4,096 and gated 2,048 -> 2 x 1,792,
+// 64 tokens, bf16 38.1 and 42.6 us against 27.0 and 36.7 and fp32 74.6 and 84.9 against 64.2 and 84.6; 32 tokens
+// 29.5 and 30.8 against 27.0 and 36.4 and 54.9 and 59.3 against 64.0 and 84.1.
 bool few_tiles(do_dtype dt, int64_t R, int32_t E, int32_t width, int cols) {
   const int64_t tiles = std::min<int64_t>(R, E) * ((width + cols - 1) / cols);
   return dol::few_rows(R, E) && tiles <= (dt == DO_F32 ? 2 : 1) * dol::device_info().cu_count;
@@ -194,7 +198,9 @@ DOLOSS_API do_status do_expert_weight_grad(const void* dy, const void* x, do_dty
   // Large against small: 64 experts of 1,536 x 1,024, 768 rows each, bf16 224 against 404 us and fp32 1,159
   // against 1,465; 16 of 1,024 x 1,024, 2,048 rows (just within the rule) 79 against 132 and 511 against 634;
   // 8 of them (outside) 112 against 124 and 973 against 621; 32 of 64 x 2,048, 8,192 rows (outside) 261
-  // against 165 and 1,955 against 641.
+  // against 165 and 1,955 against 641.  Few rows do not change that: 128 of 1,536 x 2,048, whose 1.6 GB of
+  // gradients bound it, 8 rows each 283 against 319 and 355 against 461, 128 rows 311 against 458 and 1,130
+  // against 1,463; 16 of 1,024 x 1,024, one row each 17 against 20 and 23 against 26.
   const bool big = I > 128 && O > 64 && (int64_t)E * I * O >= int64_t(256) * 65536;
   return launched((dtype == DO_F32 ? dol::launch_expert_weight_grad_f32 : dol::launch_expert_weight_grad_bf16)(
       g, big, whole(x, dtype, I, std::max(N, R)) && whole(dy, dtype, O, std::max(N, R)), stream));

@@ -26,13 +26,14 @@
 // straight to LDS write it in lane order, so it is the global address of each
 // lane that is permuted.
 //
-// 65,536 tokens of 8 of 128 experts (524,288 rows), bf16: 768 -> 2,048 in 1,660 us
-// (990 TFLOP/s), weight gradient of 1,536 x 2,048 in 3,530 to 3,620 us (910 to 940), 2,048 -> 2 x
-// 768 with the gated activation and its checkpoint in 3,300 us (1,000).  The matrix
-// cores are busy 55 % of the time at the clock of about 2 GHz that they leave; the
-// rest is the loads' way through the vector cache (a stage takes it 1.4 us, its
-// products 1.0) and the outputs at a tile's end.  fp32, 49,146 rows 1,536 -> 1,024
-// transposed: 1,260 us, 123 of the 155 TFLOP/s of a large matrix product.
+// 65,536 tokens of 8 of 128 experts (524,288 rows), bf16: 768 -> 2,048 in 1,660 to
+// 1,700 us (970 to 990 TFLOP/s), its rows' gradient from 1,536 in 3,140 us (1,050), weight
+// gradient of 1,536 x 2,048 in 3,460 to 3,640 us (910 to 950), 2,048 -> 2 x 768 with the
+// gated activation and its checkpoint in 3,300 to 3,380 us (980 to 1,000).  The matrix
+// cores are busy 55 % of the time at the clock of about 2 GHz that they leave; the rest is
+// the loads' way to LDS (a stage that the L2 cache misses takes 1.4 us, one that it holds
+// 0.63, its products 1.0) and the outputs at a tile's end.  fp32, 49,146 rows 1,536 ->
+// 1,024 transposed: 1,260 us, 123 of the 155 TFLOP/s of a large matrix product.
 #pragma once
 
 #include <atomic>
@@ -667,7 +668,8 @@ __device__ __forceinline__ void store_four(T* d, const v4f& v, int n, bool vec) 
   }
 }
 
-// 1 / (1 + e^-g), the quotient by the hardware's reciprocal (one unit in the last place off at most).
+// 1 / (1 + e^-g), the quotient by the hardware's reciprocal (one unit in the last place off at most), the
+// exponential by its power of two: about |g| units more.
 __device__ __forceinline__ float sigmoid(float g) { return __builtin_amdgcn_rcpf(1.0f + __expf(-g)); }
 
 __device__ __forceinline__ float prob_at(const ExpertGemm& g, int64_t i) {
@@ -1217,11 +1219,19 @@ hipError_t pick_gemm(const ExpertGemm& g, int size, bool vec, hipStream_t s) {
 // 16 or fewer: half as many rows as the small tile, all waves load.  A stage is 20
 // KiB, so that a CU's blocks have more of the weights on their way, which bound
 // the time (5.4 TB/s of weights).  8 of 64 experts a token, fp32, 768 -> 2,048 and
-// gated 2,048 -> 2 x 768, against the small tile: 8 rows an expert 90 and 156 us
-// against 114 and 218, 16 rows 91 and 160 against 98 and 167; 32 rows 116 and 285
-// against 126 and 225, since half of the experts then need two tiles.
+// gated 2,048 -> 2 x 768, against the small tile: 8 rows an expert 92 and 163 us
+// against 125 and 227, 16 rows 114 and 226 against 128 and 232; 32 rows 121 and 286
+// against 142 and 283, since half of the experts then need two tiles, 64 rows 221 and
+// 428 against 171 and 357.  bf16 gains little, its products being short: 8 of 128
+// experts a token, weights from memory, 1 token 13.8 and 31.8 us against 14.4 and 32.9, 16
+// tokens 47.7 and 107 against 48.8 and 107.
 //
-// Large tiles for bf16 where an expert has rows for them, small ones else: fp32's
+// Large tiles for bf16 where an expert has rows for them, small ones else.  8 of 64
+// experts a token, 768 -> 2,048, gated, and the rows' gradient 2,048 -> 768, large
+// against small: 96 rows an expert 46, 146 and 51 us against 47, 134 and 55; 128 rows 64,
+// 146 and 57 against 55, 129 and 54; 160 rows 66, 151 and 59 against 65, 144 and 62; 256
+// rows 75, 198 and 102 against 88, 203 and 85; 512 rows 122, 281 and 138 against 159, 348
+// and 178: from 96 to 256 rows neither is ahead everywhere.  fp32's
 // matrix instructions take 16 times as long, so that a small tile's loads are
 // hidden too, and it wastes less at the end of an expert's rows and of the tile
 // list (49,146 rows 1,536 -> 1,024 of 48 experts: 1,298 us against 1,468).

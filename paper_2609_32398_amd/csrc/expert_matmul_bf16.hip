@@ -1,6 +1,6 @@
 // Products of rows with their expert's weights, and with the transposed weights, bf16.
-// 524,288 rows of 128 experts, 768 -> 2,048: 1,660 us, 990 TFLOP/s, bound by the operands'
-// way to LDS.
+// 524,288 rows of 128 experts, 768 -> 2,048: 1,660 to 1,700 us, 970 to 990 TFLOP/s; transposed, 1,536 -> 2,048:
+// 3,140 us, 1,050 TFLOP/s.  Bound by the operands' way to LDS.
 #include <algorithm>
 
 #include "expert_gemm.h"

@@ -12,9 +12,11 @@
 // token's experts, of which it then visits only those that are set.
 //
 // Bound by latency and launches up to some thousand tokens (64 tokens of 8 of 128
-// experts: one block, 6.3 us); beyond, by the scattered 4-byte stores of the three
-// lists (12 N k bytes).  65,536 tokens: 128 blocks, 5.4 us for the counts of their
-// units and 45 us for the rows.
+// experts: one block, 6.5 us).  Beyond, by a row's place: a choice counts up to eight
+// words of LDS, those of neighbouring experts 64 bytes apart, so that four banks serve a
+// wave (561,000 conflict cycles at 65,536 tokens), and each block first adds up the
+// counts of all blocks.  65,536 tokens: 128 blocks, 5 us for the counts of their units and
+// 45 us for the rows, whose three lists are 6.8 MB in memory.
 #include <algorithm>
 #include <atomic>
 
@@ -212,7 +214,8 @@ template <>
 __device__ __forceinline__ uint16_t from_float<uint16_t>(float v) { return bf16_bits(v); }
 
 // y[t] = sum over the token's rows of o[row], in expert order, in fp32, rounded
-// once.  One element per thread; rows of any width and alignment.
+// once.  One element per thread; rows of any width and alignment (65,536 tokens of 8
+// rows of 2,047 bf16: 1,369 us, 1.8 TB/s, in loads of two bytes).
 template <typename T>
 __global__ __launch_bounds__(256) void k_combine(const T* o, const int32_t* token_row, int64_t N, int32_t k, int64_t R,
                                                  int32_t H, T* y) {

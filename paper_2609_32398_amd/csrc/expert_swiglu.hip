@@ -1,6 +1,6 @@
 // The experts' first product with the gated activation, and its backward pass.
-// 524,288 rows of 128 experts, 2,048 -> 2 x 768 bf16: forward with the 8-bit checkpoint 3,300 us (1,000
-// TFLOP/s), backward 2,490 us (660): half of the forward's products, and 3.2 GB of 8-bit values in and
+// 524,288 rows of 128 experts, 2,048 -> 2 x 768 bf16: forward with the 8-bit checkpoint 3,300 to 3,380 us (980 to
+// 1,000 TFLOP/s; 9 GB come from behind the L2 caches, where rows and weights are 2.9), backward 2,490 us (660): half of the forward's products, and 3.2 GB of 8-bit values in and
 // gradients out at the tiles' ends, where the matrix cores wait.
 #include <algorithm>
 

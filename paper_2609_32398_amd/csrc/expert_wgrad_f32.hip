@@ -1,6 +1,6 @@
 // Gradients of the experts' weights, fp32: sums over each expert's rows, in the order of the rows.
 // 49,152 rows of 64 experts, 1,536 x 1,024: 1,160 us, 133 of the 155 TFLOP/s of a large matrix product.
-// 3,074 rows of 8 experts, 333 x 517 (through registers): 50 us, against 30 for 352 x 512 in whole pieces: loads from odd addresses.
+// 3,074 rows of 8 experts, 333 x 517 (through registers): 48 us, against 30 for 352 x 512 in whole pieces: loads from odd addresses.
 #include <algorithm>
 
 #include "expert_gemm.h"
