@@ -18,6 +18,8 @@ Functions keep the C names:
 * ``do_expert_rows`` -> ExpertRows, and the chosen experts' products on them: ``do_expert_swiglu`` /
   ``do_expert_swiglu_grad``, ``do_expert_matmul``, ``do_expert_weight_grad``, ``do_expert_combine``
 * ``do_act8_pack`` / ``do_act8_unpack`` -> activations in 8 bits (Act8) and back
+* ``do_fp8_pack`` / ``do_fp8_unpack`` -> rows or weights in 8-bit floating point (Fp8) and back, and the experts'
+  products on them: ``do_expert_swiglu_fp8`` / ``do_expert_swiglu_grad_fp8``, ``do_expert_matmul_fp8``
 
 ``scores`` is a CUDA tensor of shape [N, E] or [L, N, E], float32 or bfloat16.
 """
@@ -92,6 +94,15 @@ def lib():
                                        vp, i64, vp], st),
             "do_act8_pack": ([vp, st, i64, i32, vp, vp, vp], st),
             "do_act8_unpack": ([vp, vp, i64, i32, vp, st, vp], st),
+            "do_fp8_pack": ([vp, st, i64, i32, vp, vp, vp], st),
+            "do_fp8_unpack": ([vp, vp, i64, i32, vp, st, vp], st),
+            "do_fp8_pack_weights": ([vp, st, i64, i32, i32, vp, vp, vp], st),
+            "do_fp8_unpack_weights": ([vp, vp, i64, i32, i32, vp, st, vp], st),
+            "do_expert_matmul_fp8": ([vp, vp, vp, vp, vp, vp, i64, i64, i32, i32, i32, i32, vp, vp], st),
+            "do_expert_swiglu_fp8": ([vp, vp, vp, vp, vp, st, vp, vp, i64, i64, i32, i32, i32, vp, vp, vp, vp, vp],
+                                     st),
+            "do_expert_swiglu_grad_fp8": ([vp, vp, vp, vp, vp, st, vp, vp, vp, vp, i64, i32, i32, i32, i32, vp, vp, vp,
+                                           vp, vp, vp, i64, vp], st),
             "do_rem_allocate": ([vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp, vp], st),
             "do_rem_dispatch": ([vp, vp, i32, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp, vp], st),
         }
@@ -574,7 +585,16 @@ class Act8(NamedTuple):
     e: torch.Tensor
 
 
+class Fp8(NamedTuple):
+    """8-bit floating point (do_fp8_pack): q float8_e4m3fn [..., W] with e uint8 [..., ceil(W / 128)], or the
+    weights q [..., O, I] with e [..., ceil(O / 128), ceil(I / 128)]."""
+
+    q: torch.Tensor
+    e: torch.Tensor
+
+
 ACT8_GROUP = 32
+FP8_BLOCK = 128
 
 
 def _row_sizes(rows: ExpertRows):
@@ -715,6 +735,13 @@ def do_expert_swiglu(x: torch.Tensor, w1: torch.Tensor, rows: ExpertRows, p: tor
     return h, kept
 
 
+def _want_checkpoint(checkpoint: Act8, R: int, F: int):
+    if not isinstance(checkpoint, Act8):
+        raise ValueError("checkpoint must be an Act8 (do_expert_swiglu with checkpoint=True)")
+    _want(checkpoint.q, "checkpoint.q", shape=(R, 2, F), dtypes=(torch.int8,))
+    _want(checkpoint.e, "checkpoint.e", shape=(R, 2, -(-F // ACT8_GROUP)), dtypes=_U8)
+
+
 def do_expert_swiglu_grad(dy: torch.Tensor, w2: torch.Tensor, rows: ExpertRows, checkpoint: Act8,
                           p: torch.Tensor | None = None):
     """(da [R, 2 F], h [R, F], dp [N, E] or None) of do_expert_swiglu followed by the second product with
@@ -726,10 +753,7 @@ def do_expert_swiglu_grad(dy: torch.Tensor, w2: torch.Tensor, rows: ExpertRows, 
     _want(w2, "w2", dtypes=_SCORE_DTYPES)
     H, F = w2.shape[1], w2.shape[2]
     _operand(dy, "dy", (N, H), w2)
-    if not isinstance(checkpoint, Act8):
-        raise ValueError("checkpoint must be an Act8 (do_expert_swiglu with checkpoint=True)")
-    _want(checkpoint.q, "checkpoint.q", shape=(R, 2, F), dtypes=(torch.int8,))
-    _want(checkpoint.e, "checkpoint.e", shape=(R, 2, -(-F // ACT8_GROUP)), dtypes=_U8)
+    _want_checkpoint(checkpoint, R, F)
     pp, pd = _probs_of(p, N, E)
     dev = w2.device
     da = torch.empty((R, 2 * F), dtype=w2.dtype, device=dev)
@@ -776,3 +800,142 @@ def do_act8_unpack(a: Act8, dtype: torch.dtype, out: torch.Tensor | None = None)
     _check(lib().do_act8_unpack(a.q.data_ptr(), a.e.data_ptr(), a.q.numel() // W, W, x.data_ptr(), _dtype_code(x),
                                 _stream()), "do_act8_unpack")
     return x
+
+
+_F8 = (torch.float8_e4m3fn,)
+
+
+def _blocks(n: int) -> int:
+    return -(-n // FP8_BLOCK)
+
+
+def _want_fp8(a: Fp8, name: str, shape, weights: bool):
+    """Checks an Fp8 operand whose values have `shape`."""
+    if not isinstance(a, Fp8):
+        raise ValueError(f"{name} must be an Fp8 (do_fp8_pack)")
+    _want(a.q, f"{name}.q", shape=shape, dtypes=_F8)
+    lead = (*shape[:-2], _blocks(shape[-2])) if weights else shape[:-1]
+    _want(a.e, f"{name}.e", shape=(*lead, _blocks(shape[-1])), dtypes=_U8)
+
+
+def _fp8_weights(w: Fp8, name: str, E: int | None):
+    """(O, I) of the weights [E, O, I] of an Fp8, after checking them."""
+    if not isinstance(w, Fp8) or not isinstance(w.q, torch.Tensor) or w.q.dim() != 3 or E not in (None, w.q.shape[0]):
+        raise ValueError(f"{name} must be an Fp8 of shape [{'E' if E is None else E}, O, I] (do_fp8_pack with weights=True)")
+    _want_fp8(w, name, tuple(w.q.shape), True)
+    return w.q.shape[1], w.q.shape[2]
+
+
+def do_fp8_pack(x: torch.Tensor, weights: bool = False) -> Fp8:
+    """x [..., W] (float32 or bfloat16) in 8-bit floating point, 128 elements of a row sharing an exponent.
+    weights: matrices x [..., O, I], 128 x 128 sharing one."""
+    if not isinstance(x, torch.Tensor) or x.dim() < (2 if weights else 1) or x.numel() == 0:
+        raise ValueError(f"x must be a tensor of shape {'[..., O, I]' if weights else '[..., W]'} with at least one element")
+    _want(x, "x", dtypes=_SCORE_DTYPES)
+    W = x.shape[-1]
+    q = torch.empty(x.shape, dtype=torch.float8_e4m3fn, device=x.device)
+    if weights:
+        O = x.shape[-2]
+        a = Fp8(q, torch.empty((*x.shape[:-2], _blocks(O), _blocks(W)), dtype=torch.uint8, device=x.device))
+        _check(lib().do_fp8_pack_weights(x.data_ptr(), _dtype_code(x), x.numel() // (O * W), O, W, q.data_ptr(),
+                                         a.e.data_ptr(), _stream()), "do_fp8_pack_weights")
+    else:
+        a = Fp8(q, torch.empty((*x.shape[:-1], _blocks(W)), dtype=torch.uint8, device=x.device))
+        _check(lib().do_fp8_pack(x.data_ptr(), _dtype_code(x), x.numel() // W, W, q.data_ptr(), a.e.data_ptr(),
+                                 _stream()), "do_fp8_pack")
+    return a
+
+
+def do_fp8_unpack(a: Fp8, dtype: torch.dtype, out: torch.Tensor | None = None) -> torch.Tensor:
+    """The values of an Fp8, rows or weights as its exponents' shape says, in float32 or bfloat16."""
+    if not isinstance(a, Fp8) or not isinstance(a.q, torch.Tensor) or a.q.dim() < 1 or a.q.numel() == 0:
+        raise ValueError("a must be an Fp8 with at least one element")
+    if dtype not in _SCORE_DTYPES:
+        raise ValueError(f"dtype {dtype} is not one of {_SCORE_DTYPES}")
+    shape = tuple(a.q.shape)
+    # one row is a block of weights as well: both forms have the same exponents
+    weights = len(shape) > 1 and isinstance(a.e, torch.Tensor) and a.e.shape[-2:-1] != shape[-2:-1]
+    _want_fp8(a, "a", shape, weights)
+    x = _out(out, "out", shape, dtype, a.q.device)
+    W = shape[-1]
+    if weights:
+        O = shape[-2]
+        _check(lib().do_fp8_unpack_weights(a.q.data_ptr(), a.e.data_ptr(), a.q.numel() // (O * W), O, W, x.data_ptr(),
+                                           _dtype_code(x), _stream()), "do_fp8_unpack_weights")
+    else:
+        _check(lib().do_fp8_unpack(a.q.data_ptr(), a.e.data_ptr(), a.q.numel() // W, W, x.data_ptr(), _dtype_code(x),
+                                   _stream()), "do_fp8_unpack")
+    return x
+
+
+def do_expert_matmul_fp8(x: Fp8, w: Fp8, rows: ExpertRows | None, gather: bool = False, transposed: bool = False,
+                         out: torch.Tensor | None = None) -> torch.Tensor:
+    """do_expert_matmul on 8-bit rows x and weights w [E, O, I]: y bfloat16 [R, O] (transposed: [R, I]).  rows None:
+    one matrix w [1, O, I] for all rows of x."""
+    if rows is None:
+        if gather:
+            raise ValueError("gather needs rows")
+        O, I = _fp8_weights(w, "w", 1)
+        if not isinstance(x, Fp8) or not isinstance(x.q, torch.Tensor) or x.q.dim() != 2 or x.q.numel() == 0:
+            raise ValueError("x must be an Fp8 of shape [R, O or I]")
+        N = R = x.q.shape[0]
+        E = 1
+    else:
+        N, E, k, R = _row_sizes(rows)
+        O, I = _fp8_weights(w, "w", E)
+    _want_fp8(x, "x", (N if gather else R, O if transposed else I), False)
+    y = _out(out, "out", (R, I if transposed else O), torch.bfloat16, w.q.device)
+    _check(lib().do_expert_matmul_fp8(x.q.data_ptr(), x.e.data_ptr(), w.q.data_ptr(), w.e.data_ptr(),
+                                      rows.offsets.data_ptr() if rows is not None else None,
+                                      rows.row_token.data_ptr() if gather else None, N, R, E, O, I, int(transposed),
+                                      y.data_ptr(), _stream()), "do_expert_matmul_fp8")
+    return y
+
+
+def do_expert_swiglu_fp8(x: Fp8, w1: Fp8, rows: ExpertRows, p: torch.Tensor | None = None, checkpoint: bool = False):
+    """do_expert_swiglu on 8-bit tokens x [N, H] and weights w1 [E, 2 F, H]: (h, checkpoint) with h an Fp8 of [R, F]."""
+    N, E, k, R = _row_sizes(rows)
+    F2, H = _fp8_weights(w1, "w1", E)
+    if F2 % 2:
+        raise ValueError(f"w1 must have shape [{E}, 2 F, H]")
+    F = F2 // 2
+    _want_fp8(x, "x", (N, H), False)
+    pp, pd = _probs_of(p, N, E)
+    dev = w1.q.device
+    h = Fp8(torch.empty((R, F), dtype=torch.float8_e4m3fn, device=dev),
+            torch.empty((R, _blocks(F)), dtype=torch.uint8, device=dev))
+    kept = None
+    if checkpoint:
+        kept = Act8(torch.empty((R, 2, F), dtype=torch.int8, device=dev),
+                    torch.empty((R, 2, -(-F // ACT8_GROUP)), dtype=torch.uint8, device=dev))
+    _check(lib().do_expert_swiglu_fp8(x.q.data_ptr(), x.e.data_ptr(), w1.q.data_ptr(), w1.e.data_ptr(), pp, pd,
+                                      rows.offsets.data_ptr(), rows.row_token.data_ptr(), N, R, E, H, F,
+                                      h.q.data_ptr(), h.e.data_ptr(), kept.q.data_ptr() if kept else None,
+                                      kept.e.data_ptr() if kept else None, _stream()), "do_expert_swiglu_fp8")
+    return h, kept
+
+
+def do_expert_swiglu_grad_fp8(dy: Fp8, w2: Fp8, rows: ExpertRows, checkpoint: Act8, p: torch.Tensor | None = None):
+    """do_expert_swiglu_grad on an 8-bit gradient dy [N, H] and weights w2 [E, H, F]: (da, h, dp), da and h bfloat16."""
+    N, E, k, R = _row_sizes(rows)
+    H, F = _fp8_weights(w2, "w2", E)
+    _want_fp8(dy, "dy", (N, H), False)
+    _want_checkpoint(checkpoint, R, F)
+    pp, pd = _probs_of(p, N, E)
+    dev = w2.q.device
+    da = torch.empty((R, 2 * F), dtype=torch.bfloat16, device=dev)
+    h = torch.empty((R, F), dtype=torch.bfloat16, device=dev)
+    dp = ws = None
+    need = 0
+    if p is not None:
+        dp = torch.empty((N, E), dtype=p.dtype, device=dev)
+        need = lib().do_expert_swiglu_grad_workspace(R, F)
+        ws = torch.empty(need, dtype=torch.uint8, device=dev)
+    _check(lib().do_expert_swiglu_grad_fp8(dy.q.data_ptr(), dy.e.data_ptr(), w2.q.data_ptr(), w2.e.data_ptr(), pp, pd,
+                                           rows.offsets.data_ptr(), rows.row_token.data_ptr(),
+                                           rows.token_row.data_ptr(), rows.token_expert.data_ptr(), N, E, k, H, F,
+                                           checkpoint.q.data_ptr(), checkpoint.e.data_ptr(), da.data_ptr(),
+                                           h.data_ptr(), dp.data_ptr() if dp is not None else None,
+                                           ws.data_ptr() if ws is not None else None, need, _stream()),
+           "do_expert_swiglu_grad_fp8")
+    return da, h, dp

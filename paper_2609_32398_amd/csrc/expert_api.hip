@@ -262,33 +262,36 @@ DOLOSS_API int64_t do_expert_swiglu_grad_workspace(int64_t R, int32_t F) {
   return R < 1 || F < 1 ? 0 : R * ((F + 63) / 64) * (int64_t)sizeof(float);
 }
 
-DOLOSS_API do_status do_expert_swiglu_grad(const void* dy, const void* w2, do_dtype dtype, const void* p,
-                                           do_dtype p_dtype, const int32_t* offsets, const int32_t* row_token,
-                                           const int32_t* token_row, const int32_t* token_expert, int64_t N, int32_t E,
-                                           int32_t k, int32_t H, int32_t F, const int8_t* q, const uint8_t* e,
-                                           void* da, void* h, void* dp, void* workspace, int64_t workspace_bytes,
-                                           hipStream_t stream) {
+namespace {
+
+// What the backward passes check alike; dtype is that of da and h.
+do_status check_grad(do_dtype dtype, const void* p, do_dtype p_dtype, const int32_t* offsets, const int32_t* row_token,
+                     const int32_t* token_row, const int32_t* token_expert, int64_t N, int32_t E, int32_t k, int32_t H,
+                     int32_t F, const int8_t* q, const uint8_t* e, const void* da, const void* h, const void* dp,
+                     const void* workspace, int64_t workspace_bytes) {
   DO_TRY(check_experts(N, E, k));
   const int64_t R = N * k;
   DO_TRY(check_swiglu(dtype, p, p_dtype, offsets, row_token, N, R, E, H, F));
-  DO_TRY(check_ptr(dy, size_of(dtype), "dy is NULL or not aligned to its element size"));
-  DO_TRY(check_ptr(w2, size_of(dtype), "w2 is NULL or not aligned to its element size"));
   DO_TRY(check_ptr(da, size_of(dtype), "da is NULL or not aligned to its element size"));
   DO_TRY(check_ptr(h, size_of(dtype), "h is NULL or not aligned to its element size"));
   DO_TRY(check_ptr(q, 1, "q is NULL"));
   DO_TRY(check_ptr(e, 1, "e is NULL"));
-  if (dp != nullptr) {
-    if (p == nullptr) return set_error(DO_ERR_INVALID_ARG, "dp is the gradient of p, which is NULL");
-    if (!aligned(dp, size_of(p_dtype))) return set_error(DO_ERR_INVALID_ARG, "dp is not aligned to its element size");
-    DO_TRY(check_ptr(token_row, 4, "token_row is NULL or not 4-byte aligned"));
-    DO_TRY(check_ptr(token_expert, 4, "token_expert is NULL or not 4-byte aligned"));
-    DO_TRY(check_ptr(workspace, 4, "workspace is NULL or not 4-byte aligned"));
-    if (workspace_bytes < do_expert_swiglu_grad_workspace(R, F))
-      return set_error(DO_ERR_INVALID_ARG, "workspace is smaller than do_expert_swiglu_grad_workspace(R, F)");
-  }
+  if (dp == nullptr) return DO_OK;
+  if (p == nullptr) return set_error(DO_ERR_INVALID_ARG, "dp is the gradient of p, which is NULL");
+  if (!aligned(dp, size_of(p_dtype))) return set_error(DO_ERR_INVALID_ARG, "dp is not aligned to its element size");
+  DO_TRY(check_ptr(token_row, 4, "token_row is NULL or not 4-byte aligned"));
+  DO_TRY(check_ptr(token_expert, 4, "token_expert is NULL or not 4-byte aligned"));
+  DO_TRY(check_ptr(workspace, 4, "workspace is NULL or not 4-byte aligned"));
+  if (workspace_bytes < do_expert_swiglu_grad_workspace(R, F))
+    return set_error(DO_ERR_INVALID_ARG, "workspace is smaller than do_expert_swiglu_grad_workspace(R, F)");
+  return DO_OK;
+}
+
+// The backward passes' products but for their operands.
+dol::ExpertGemm grad_of(const void* p, do_dtype p_dtype, const int32_t* offsets, const int32_t* row_token, int64_t N,
+                        int64_t R, int32_t E, int32_t H, int32_t F, const int8_t* q, const uint8_t* e, void* da,
+                        void* h, const void* dp, void* workspace) {
   dol::ExpertGemm g{};
-  g.P = w2;
-  g.Q = dy;
   g.offsets = offsets;
   g.q_token = row_token;
   g.N = N;
@@ -298,7 +301,6 @@ DOLOSS_API do_status do_expert_swiglu_grad(const void* dy, const void* w2, do_dt
   g.K = H;
   g.ldp = F;
   g.ldq = H;
-  g.wide = wide(dtype, H, N);
   g.prob = p;
   g.p_bf16 = p_dtype == DO_BF16;
   g.q8 = const_cast<int8_t*>(q);
@@ -308,9 +310,30 @@ DOLOSS_API do_status do_expert_swiglu_grad(const void* dy, const void* w2, do_dt
   g.dp = dp != nullptr ? static_cast<float*>(workspace) : nullptr;
   g.vec_out = aligned(da, 16) && aligned(h, 16) && F % 8 == 0;
   g.vec_q8 = aligned(q, 16) && F % 16 == 0;
+  return g;
+}
+
+}  // namespace
+
+DOLOSS_API do_status do_expert_swiglu_grad(const void* dy, const void* w2, do_dtype dtype, const void* p,
+                                           do_dtype p_dtype, const int32_t* offsets, const int32_t* row_token,
+                                           const int32_t* token_row, const int32_t* token_expert, int64_t N, int32_t E,
+                                           int32_t k, int32_t H, int32_t F, const int8_t* q, const uint8_t* e,
+                                           void* da, void* h, void* dp, void* workspace, int64_t workspace_bytes,
+                                           hipStream_t stream) {
+  DO_TRY(check_dtype(dtype));
+  DO_TRY(check_ptr(dy, size_of(dtype), "dy is NULL or not aligned to its element size"));
+  DO_TRY(check_ptr(w2, size_of(dtype), "w2 is NULL or not aligned to its element size"));
+  DO_TRY(check_grad(dtype, p, p_dtype, offsets, row_token, token_row, token_expert, N, E, k, H, F, q, e, da, h, dp,
+                    workspace, workspace_bytes));
+  dol::ExpertGemm g = grad_of(p, p_dtype, offsets, row_token, N, N * k, E, H, F, q, e, da, h, dp, workspace);
+  g.P = w2;
+  g.Q = dy;
+  g.wide = wide(dtype, H, N);
   DO_TRY(launched(dol::launch_expert_swiglu_grad(g, dtype, whole(dy, dtype, H, N) && whole(w2, dtype, F), stream)));
   if (dp == nullptr) return DO_OK;
-  return launched(dol::launch_expert_dp(g.dp, (F + 63) / 64, R, token_row, token_expert, N, k, E, dp, p_dtype, stream));
+  return launched(
+      dol::launch_expert_dp(g.dp, (F + 63) / 64, g.R, token_row, token_expert, N, k, E, dp, p_dtype, stream));
 }
 
 DOLOSS_API do_status do_act8_pack(const void* x, do_dtype dtype, int64_t rows, int32_t W, int8_t* q, uint8_t* e,
@@ -333,4 +356,161 @@ DOLOSS_API do_status do_act8_unpack(const int8_t* q, const uint8_t* e, int64_t r
   DO_TRY(check_ptr(e, 1, "e is NULL"));
   DO_TRY(check_ptr(x, size_of(dtype), "x is NULL or not aligned to its element size"));
   return launched(dol::launch_act8_unpack(q, e, rows, W, x, dtype, stream));
+}
+
+// ---- 8-bit floating point -----------------------------------------------------
+
+namespace {
+
+// Operands of 8-bit values: one byte an element.
+bool whole8(const uint8_t* p, int32_t row, int64_t rows = 1) {
+  return aligned(p, 16) && row % 16 == 0 && rows * (row / 16) < (int64_t(1) << 32);
+}
+
+do_status check_fp8(const uint8_t* q, const uint8_t* e, const char* msg) {
+  return q == nullptr || e == nullptr ? set_error(DO_ERR_INVALID_ARG, msg) : DO_OK;
+}
+
+do_status check_matrices(int64_t mats, int64_t O, int32_t I) {
+  DO_TRY(check_rows(1, mats, 1, (int64_t(1) << 31) - 1));
+  if (O < 1 || O > 2 * (int64_t)dol::kMaxWidth || I < 1 || I > dol::kMaxWidth)
+    return set_error(DO_ERR_INVALID_ARG, "O must be in [1, 131072] and I in [1, 65536]");
+  if (mats * ((O + 127) / 128) * ((I + 127) / 128) >= (int64_t(1) << 31))
+    return set_error(DO_ERR_OVERFLOW, "2^31 blocks of weights or more");
+  return DO_OK;
+}
+
+}  // namespace
+
+DOLOSS_API do_status do_fp8_pack(const void* x, do_dtype dtype, int64_t rows, int32_t W, uint8_t* q, uint8_t* e,
+                                 hipStream_t stream) {
+  DO_TRY(check_dtype(dtype));
+  DO_TRY(check_rows(1, rows, 1, (int64_t(1) << 31) - 1));
+  DO_TRY(check_widths(1, 1, {W}));
+  DO_TRY(check_ptr(x, size_of(dtype), "x is NULL or not aligned to its element size"));
+  DO_TRY(check_fp8(q, e, "q or e is NULL"));
+  return launched(dol::launch_fp8_pack(x, dtype, 1, rows, W, false, q, e, stream));
+}
+
+DOLOSS_API do_status do_fp8_unpack(const uint8_t* q, const uint8_t* e, int64_t rows, int32_t W, void* x,
+                                   do_dtype dtype, hipStream_t stream) {
+  DO_TRY(check_dtype(dtype));
+  DO_TRY(check_rows(1, rows, 1, (int64_t(1) << 31) - 1));
+  DO_TRY(check_widths(1, 1, {W}));
+  DO_TRY(check_fp8(q, e, "q or e is NULL"));
+  DO_TRY(check_ptr(x, size_of(dtype), "x is NULL or not aligned to its element size"));
+  return launched(dol::launch_fp8_unpack(q, e, 1, rows, W, false, x, dtype, stream));
+}
+
+DOLOSS_API do_status do_fp8_pack_weights(const void* w, do_dtype dtype, int64_t mats, int32_t O, int32_t I, uint8_t* q,
+                                         uint8_t* e, hipStream_t stream) {
+  DO_TRY(check_dtype(dtype));
+  DO_TRY(check_matrices(mats, O, I));
+  DO_TRY(check_ptr(w, size_of(dtype), "w is NULL or not aligned to its element size"));
+  DO_TRY(check_fp8(q, e, "q or e is NULL"));
+  return launched(dol::launch_fp8_pack(w, dtype, mats, O, I, true, q, e, stream));
+}
+
+DOLOSS_API do_status do_fp8_unpack_weights(const uint8_t* q, const uint8_t* e, int64_t mats, int32_t O, int32_t I,
+                                           void* w, do_dtype dtype, hipStream_t stream) {
+  DO_TRY(check_dtype(dtype));
+  DO_TRY(check_matrices(mats, O, I));
+  DO_TRY(check_fp8(q, e, "q or e is NULL"));
+  DO_TRY(check_ptr(w, size_of(dtype), "w is NULL or not aligned to its element size"));
+  return launched(dol::launch_fp8_unpack(q, e, mats, O, I, true, w, dtype, stream));
+}
+
+DOLOSS_API do_status do_expert_matmul_fp8(const uint8_t* x, const uint8_t* x_exp, const uint8_t* w,
+                                          const uint8_t* w_exp, const int32_t* offsets, const int32_t* row_token,
+                                          int64_t N, int64_t R, int32_t E, int32_t O, int32_t I, int32_t transposed,
+                                          void* y, hipStream_t stream) {
+  DO_TRY(check_rows(N, R, E));
+  DO_TRY(check_widths(R, E, {O, I}));
+  DO_TRY(check_fp8(x, x_exp, "x or its exponents are NULL"));
+  DO_TRY(check_fp8(w, w_exp, "w or its exponents are NULL"));
+  DO_TRY(check_ptr(y, 2, "y is NULL or not aligned to its element size"));
+  if (offsets == nullptr && E != 1) return set_error(DO_ERR_INVALID_ARG, "offsets is NULL, which one expert alone allows");
+  if (!aligned(offsets, 4) || !aligned(row_token, 4))
+    return set_error(DO_ERR_INVALID_ARG, "offsets or row_token is not 4-byte aligned");
+  const int32_t in = transposed ? O : I, out = transposed ? I : O;
+  dol::ExpertGemm g{};
+  g.P = w;
+  g.Q = x;
+  g.p_exp = w_exp;
+  g.q_exp = x_exp;
+  g.offsets = offsets;
+  g.q_token = row_token;
+  g.N = N;
+  g.R = R;
+  g.E = E;
+  g.Pd = out;
+  g.K = in;
+  g.ldp = I;
+  g.ldq = in;
+  g.out = y;
+  g.wide = row_token != nullptr && N * in >= (int64_t(1) << 32);
+  g.vec_out = aligned(y, 16) && out % 8 == 0;
+  const bool vec = (transposed ? whole8(w, I) : whole8(w, I) && (int64_t)O * I < (int64_t(1) << 32)) &&
+                   whole8(x, in, row_token != nullptr ? N : R);
+  return launched(dol::launch_expert_matmul_fp8(g, transposed != 0, vec, stream));
+}
+
+DOLOSS_API do_status do_expert_swiglu_fp8(const uint8_t* x, const uint8_t* x_exp, const uint8_t* w1,
+                                          const uint8_t* w1_exp, const void* p, do_dtype p_dtype,
+                                          const int32_t* offsets, const int32_t* row_token, int64_t N, int64_t R,
+                                          int32_t E, int32_t H, int32_t F, uint8_t* h, uint8_t* h_exp, int8_t* q,
+                                          uint8_t* e, hipStream_t stream) {
+  DO_TRY(check_swiglu(DO_BF16, p, p_dtype, offsets, row_token, N, R, E, H, F));
+  DO_TRY(check_fp8(x, x_exp, "x or its exponents are NULL"));
+  DO_TRY(check_fp8(w1, w1_exp, "w1 or its exponents are NULL"));
+  DO_TRY(check_fp8(h, h_exp, "h or its exponents are NULL"));
+  if ((q == nullptr) != (e == nullptr)) return set_error(DO_ERR_INVALID_ARG, "q and e are given together or not at all");
+  dol::ExpertGemm g{};
+  g.P = w1;
+  g.Q = x;
+  g.p_exp = w1_exp;
+  g.q_exp = x_exp;
+  g.offsets = offsets;
+  g.q_token = row_token;
+  g.N = N;
+  g.R = R;
+  g.E = E;
+  g.Pd = F;
+  g.K = H;
+  g.ldp = H;
+  g.ldq = H;
+  g.wide = N * H >= (int64_t(1) << 32);
+  g.prob = p;
+  g.p_bf16 = p_dtype == DO_BF16;
+  g.q8 = q;
+  g.e8 = e;
+  g.out = h;
+  g.h_exp = h_exp;
+  g.vec_out = aligned(h, 16) && F % 16 == 0;
+  g.vec_q8 = q != nullptr && aligned(q, 16) && F % 16 == 0;
+  const bool vec = whole8(x, H, N) && whole8(w1, H) && 2 * (int64_t)F * H < (int64_t(1) << 32);
+  return launched(dol::launch_expert_swiglu_fp8(g, vec, stream));
+}
+
+DOLOSS_API do_status do_expert_swiglu_grad_fp8(const uint8_t* dy, const uint8_t* dy_exp, const uint8_t* w2,
+                                               const uint8_t* w2_exp, const void* p, do_dtype p_dtype,
+                                               const int32_t* offsets, const int32_t* row_token,
+                                               const int32_t* token_row, const int32_t* token_expert, int64_t N,
+                                               int32_t E, int32_t k, int32_t H, int32_t F, const int8_t* q,
+                                               const uint8_t* e, void* da, void* h, void* dp, void* workspace,
+                                               int64_t workspace_bytes, hipStream_t stream) {
+  DO_TRY(check_fp8(dy, dy_exp, "dy or its exponents are NULL"));
+  DO_TRY(check_fp8(w2, w2_exp, "w2 or its exponents are NULL"));
+  DO_TRY(check_grad(DO_BF16, p, p_dtype, offsets, row_token, token_row, token_expert, N, E, k, H, F, q, e, da, h, dp,
+                    workspace, workspace_bytes));
+  dol::ExpertGemm g = grad_of(p, p_dtype, offsets, row_token, N, N * k, E, H, F, q, e, da, h, dp, workspace);
+  g.P = w2;
+  g.Q = dy;
+  g.p_exp = w2_exp;
+  g.q_exp = dy_exp;
+  g.wide = N * H >= (int64_t(1) << 32);
+  DO_TRY(launched(dol::launch_expert_swiglu_grad_fp8(g, whole8(dy, H, N) && whole8(w2, F), stream)));
+  if (dp == nullptr) return DO_OK;
+  return launched(
+      dol::launch_expert_dp(g.dp, (F + 63) / 64, g.R, token_row, token_expert, N, k, E, dp, p_dtype, stream));
 }

@@ -8,6 +8,7 @@
 namespace dol {
 
 constexpr int kAct8Group = 32;          // elements that share one exponent byte
+constexpr int kFp8Block = 128;          // the same of 8-bit floating point (weights: 128 x 128)
 constexpr int32_t kMaxWidth = 1 << 16;  // of a row of activations or weights
 // Rows of a product: a tile's rows, a stage and a list of 1,024 tokens are added to a row's number in int32.
 constexpr int64_t kMaxRows = (int64_t(1) << 31) - 1024;
@@ -52,6 +53,9 @@ struct ExpertGemm {
   uint8_t* e8;             // [R][2][G] their exponents
   void* out;
   void* out2;              // backward pass: the activations again
+  const uint8_t* p_exp;    // 8-bit floating point: the operands' exponents (of the weights', and of the rows' blocks)
+  const uint8_t* q_exp;
+  uint8_t* h_exp;          // and those of the activations
   float* dp;               // backward pass: partial sums of the probabilities' gradient, [R][ceil(F / 64)]
 };
 
@@ -60,6 +64,15 @@ hipError_t launch_expert_matmul_f32(const ExpertGemm& g, bool transposed, bool v
 hipError_t launch_expert_weight_grad_bf16(const ExpertGemm& g, bool big, bool vec, hipStream_t s);
 hipError_t launch_expert_weight_grad_f32(const ExpertGemm& g, bool big, bool vec, hipStream_t s);
 hipError_t launch_expert_swiglu(const ExpertGemm& g, do_dtype dt, bool vec, hipStream_t s);
+// In 8 bits (p_exp, q_exp); offsets may be NULL: one expert with all R rows.
+hipError_t launch_expert_matmul_fp8(const ExpertGemm& g, bool transposed, bool vec, hipStream_t s);
+hipError_t launch_expert_swiglu_fp8(const ExpertGemm& g, bool vec, hipStream_t s);
+hipError_t launch_expert_swiglu_grad_fp8(const ExpertGemm& g, bool vec, hipStream_t s);
+// Matrices of weights [mats][O][I] (weights), or rows [mats * O][I], to 8 bits and back.
+hipError_t launch_fp8_pack(const void* x, do_dtype dt, int64_t mats, int64_t O, int32_t I, bool weights, uint8_t* q,
+                           uint8_t* e, hipStream_t s);
+hipError_t launch_fp8_unpack(const uint8_t* q, const uint8_t* e, int64_t mats, int64_t O, int32_t I, bool weights,
+                             void* x, do_dtype dt, hipStream_t s);
 hipError_t launch_expert_swiglu_grad(const ExpertGemm& g, do_dtype dt, bool vec, hipStream_t s);
 // 16 rows an expert or fewer on average.
 inline bool few_rows(int64_t R, int32_t E) { return R / E <= 16; }
@@ -111,6 +124,25 @@ __device__ __forceinline__ uint32_t act8_round4(const float* x, float inv, uint3
   const uint32_t lo = __builtin_amdgcn_perm(b[1], b[0], 0x0C0C0400u), hi = __builtin_amdgcn_perm(b[3], b[2], 0x04000C0Cu);
   return byte == 255u ? 0u : lo | hi;
 }
+// 8-bit floating point (e4m3: 3 bits after the leading one, 448 at most).  Exponent byte of a block whose largest
+// magnitude has the bit pattern m: the least e >= -120 with amax <= 448 * 2^e, plus 127; 255 when it holds an infinity
+// or NaN.  448 is 1.75 * 2^8, whose mantissa bits are 0x600000.  -120 leaves 2^-9 2^e, the least step, to fp32's range
+// on both sides (2^-e is used too).
+__device__ __forceinline__ uint32_t fp8_exponent(uint32_t m) {
+  if (m >= 0x7F800000u) return 255u;
+  const int e = (int)(m >> 23) - 8 + ((m & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+  return (uint32_t)(e < 7 ? 7 : e);
+}
+__device__ __forceinline__ float fp8_inverse(uint32_t byte) { return act8_inverse(byte); }
+__device__ __forceinline__ float fp8_scale(uint32_t byte) { return act8_scale(byte); }
+// Four values within 448, each rounded once to e4m3 (nearest, ties to even), one to a byte; 0 in a block that is not
+// finite.
+__device__ __forceinline__ uint32_t fp8_round4(float a, float b, float c, float d, uint32_t byte) {
+  int v = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  v = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, v, true);
+  return byte == 255u ? 0u : (uint32_t)v;
+}
+
 // Four 8-bit values times s = 2^e, exactly.
 __device__ __forceinline__ void act8_values4(uint32_t q, float s, float* v) {
   const uint32_t u = q ^ 0x80808080u;  // + 128: unsigned bytes convert in one instruction

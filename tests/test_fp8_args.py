@@ -1,0 +1,83 @@
+"""Refusals of the 8-bit floating point entry points: on the host, before any GPU work."""
+import os
+
+import pytest
+import torch
+
+from test_expert_args import FAKE, _rejects
+
+E4M3 = torch.float8_e4m3fn
+
+
+@pytest.fixture(scope="module")
+def dl():
+    import paper_2609_32398_amd as p
+
+    if not os.path.exists(p.LIB_PATH):
+        p.build()
+    return p
+
+
+def test_pack_and_unpack(dl):
+    _rejects(dl, "do_fp8_pack", [FAKE, 0, 10, 64, FAKE, FAKE, None], [
+        (0, None, 1), (0, FAKE + 2, 1), (1, 2, 2), (2, 0, 1), (2, 1 << 31, 4), (3, 0, 1), (3, 65537, 1), (4, None, 1),
+        (5, None, 1)])
+    _rejects(dl, "do_fp8_unpack", [FAKE, FAKE, 10, 64, FAKE, 1, None], [
+        (0, None, 1), (1, None, 1), (2, -1, 1), (2, 1 << 31, 4), (3, 0, 1), (4, None, 1), (4, FAKE + 1, 1), (5, 7, 2)])
+    changes = [(2, 0, 1), (2, 1 << 31, 4), (3, 0, 1), (3, 131073, 1), (4, 0, 1), (4, 65537, 1),
+               ((2, 3, 4), (1 << 30, 129, 128), 4)]
+    _rejects(dl, "do_fp8_pack_weights", [FAKE, 1, 2, 64, 64, FAKE, FAKE, None],
+             changes + [(0, None, 1), (0, FAKE + 1, 1), (1, 9, 2), (5, None, 1), (6, None, 1)])
+    _rejects(dl, "do_fp8_unpack_weights", [FAKE, FAKE, 2, 64, 64, FAKE, 0, None],
+             changes + [(0, None, 1), (1, None, 1), (5, None, 1), (5, FAKE + 2, 1), (6, 9, 2)])
+
+
+def test_products(dl):
+    _rejects(dl, "do_expert_matmul_fp8", [FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, 10, 20, 4, 64, 64, 0, FAKE, None], [
+        (0, None, 1), (1, None, 1), (2, None, 1), (3, None, 1), (4, None, 1), (4, FAKE + 2, 1), (5, FAKE + 1, 1),
+        (6, 0, 1), (6, 1 << 31, 4), (7, 0, 1), (7, (1 << 31) - 1000, 4), (8, 0, 1), (8, 1025, 1), (9, 0, 1),
+        (9, 65537, 1), (10, 0, 1), (10, 65537, 1), (12, None, 1), (12, FAKE + 1, 1),
+        ((4, 7, 8, 9), (None, (1 << 31) - 1025, 1, 65536), 4)])
+    _rejects(dl, "do_expert_swiglu_fp8",
+             [FAKE, FAKE, FAKE, FAKE, FAKE, 1, FAKE, FAKE, 10, 20, 4, 64, 64, FAKE, FAKE, FAKE, FAKE, None], [
+                 (0, None, 1), (1, None, 1), (2, None, 1), (3, None, 1), (4, FAKE + 1, 1), (5, 3, 2), (6, None, 1),
+                 (7, None, 1), (8, 0, 1), (9, 0, 1), (10, 0, 1), (11, 0, 1), (12, 65537, 1), (13, None, 1),
+                 (14, None, 1), (15, None, 1), (16, None, 1)])
+    good = [FAKE, FAKE, FAKE, FAKE, FAKE, 1, FAKE, FAKE, FAKE, FAKE, 10, 4, 2, 64, 64, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE,
+            20 * 4, None]
+    _rejects(dl, "do_expert_swiglu_grad_fp8", good, [
+        (0, None, 1), (1, None, 1), (2, None, 1), (3, None, 1), (4, None, 1), (4, FAKE + 1, 1), (5, 3, 2), (6, None, 1),
+        (7, None, 1), (8, None, 1), (9, None, 1), (10, 0, 1), (11, 0, 1), (12, 5, 1), (13, 0, 1), (14, 0, 1),
+        (15, None, 1), (16, None, 1), (17, None, 1), (17, FAKE + 1, 1), (18, None, 1), (19, FAKE + 1, 1), (20, None, 1),
+        (21, 79, 1)])
+
+
+def _fp8(dl, *shape, e=None, dtype=E4M3):
+    return dl.Fp8(torch.zeros(shape, dtype=dtype), torch.zeros(e or (*shape[:-1], -(-shape[-1] // 128)), dtype=torch.uint8))
+
+
+def _refused(f, *args, say=None, **kw):
+    with pytest.raises(ValueError) as err:
+        f(*args, **kw)
+    assert say is None or say in str(err.value), err.value
+
+
+def test_binding(dl):
+    # shapes and types are looked at before the device, so that CPU tensors show them
+    rows = dl.ExpertRows(torch.zeros(5, dtype=torch.int32), torch.zeros(20, dtype=torch.int32),
+                         torch.zeros(10, 2, dtype=torch.int32), torch.zeros(10, 2, dtype=torch.int32))
+    _refused(dl.do_fp8_pack, torch.zeros(0, 4), say="at least one")
+    _refused(dl.do_fp8_pack, torch.zeros(4), weights=True, say="[..., O, I]")
+    _refused(dl.do_fp8_pack, torch.zeros(4, dtype=torch.float16), say="dtype")
+    _refused(dl.do_fp8_pack, torch.zeros(4, 6)[:, ::2], say="contiguous")
+    _refused(dl.do_fp8_pack, torch.zeros(4, 6), say="device tensor")
+    _refused(dl.do_fp8_unpack, (1, 2), torch.float32, say="Fp8")
+    _refused(dl.do_fp8_unpack, _fp8(dl, 4, 200), torch.float16, say="dtype")
+    _refused(dl.do_fp8_unpack, _fp8(dl, 4, 200, e=(4, 1)), torch.float32, say="device")  # q's device comes first
+    _refused(dl.do_fp8_unpack, dl.Fp8(None, None), torch.float32, say="Fp8")
+    _refused(dl.do_expert_matmul_fp8, _fp8(dl, 10, 64), _fp8(dl, 1, 32, 64, e=(1, 1, 1)), None, gather=True, say="gather")
+    _refused(dl.do_expert_matmul_fp8, _fp8(dl, 10, 64), _fp8(dl, 2, 32, 64, e=(2, 1, 1)), None, say="[1, O, I]")
+    _refused(dl.do_expert_matmul_fp8, torch.zeros(10, 64), _fp8(dl, 1, 32, 64, e=(1, 1, 1)), None)
+    _refused(dl.do_expert_matmul_fp8, _fp8(dl, 20, 64), _fp8(dl, 4, 32, 64, e=(4, 1, 1)), "rows", say="ExpertRows")
+    _refused(dl.do_expert_swiglu_fp8, _fp8(dl, 10, 64), torch.zeros(4, 32, 64), rows)
+    _refused(dl.do_expert_swiglu_grad_fp8, _fp8(dl, 10, 64), torch.zeros(4, 64, 32), rows, None)

@@ -1,0 +1,463 @@
+"""The experts' products in 8-bit floating point against plain forms in 64 bits.
+
+Operands are small whole numbers times powers of two (fp8_util.lattice), whose products and sums are exact in the
+matrix instructions, so that a product has to be its rounding to bf16 exactly; normal ones follow with a bound.
+"""
+import pytest
+import torch
+
+from expert_util import EPS16, EPS32, choose, device_rows, product_tol, spans, within
+from fp8_util import BLOCK, E4M3, TINY, blocks, eight_bit_tol, lattice, power, same, spread, values
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+@pytest.fixture(scope="module")
+def dl():
+    import paper_2609_32398_amd as p
+
+    return p
+
+
+def _gen(seed):
+    g = torch.Generator()
+    g.manual_seed(seed)
+    return g
+
+
+def _products(x, w, mask, k, transposed, R):
+    """Rows x [R][..] (64 bits) times their expert's weights, and the sums of the magnitudes."""
+    ref = torch.zeros(R, w.shape[2 if transposed else 1], dtype=torch.float64, device="cuda")
+    size = torch.zeros_like(ref)
+    for e, a, b, _ in spans(mask, k):
+        we = w[e] if transposed else w[e].t()
+        ref[a:b] = x[a:b] @ we
+        size[a:b] = x[a:b].abs() @ we.abs()
+    return ref, size
+
+
+# --- products --------------------------------------------------------------------------------------------------------
+
+# N, E, k, O, I: every tile, widths of whole pieces and not, single tokens, contractions below, at and past one and
+# four blocks, experts with no row, one and most of them
+SHAPES = [(1, 8, 2, 64, 64), (1, 128, 8, 96, 40), (3, 4, 1, 1, 1), (70, 8, 2, 33, 7), (200, 16, 4, 130, 96),
+          (129, 8, 3, 200, 264), (700, 4, 2, 256, 128), (700, 4, 2, 300, 72), (1000, 3, 2, 257, 129),
+          (900, 5, 2, 528, 656), (64, 256, 8, 72, 200), (2500, 2, 1, 64, 512), (300, 8, 2, 1040, 144),
+          (1500, 4, 2, 1296, 1024), (9, 4, 2, 384, 1152)]
+
+
+@pytest.mark.parametrize("N,E,k,O,I", SHAPES)
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("dist,gather", [("even", False), ("idle", True), ("one", True)])
+def test_matmul_is_exact(dl, N, E, k, O, I, transposed, dist, gather):
+    print(f"[case] matmul fp8 N={N} E={E} k={k} O={O} I={I} t={transposed} {dist} gather={gather}", flush=True)
+    gen = _gen(N + O + I)
+    mask = choose(gen, N, E, k, dist)
+    rows = device_rows(dl, mask, k)
+    R, inner = N * k, O if transposed else I
+    w = lattice(dl, gen, E, O, I, weights=True)
+    x = lattice(dl, gen, N if gather else R, inner)
+    y = dl.do_expert_matmul_fp8(x, w, rows, gather=gather, transposed=transposed)
+    v = values(x)
+    ref, _ = _products(v[rows.row_token.long()] if gather else v, values(w, True), mask, k, transposed, R)
+    assert y.dtype == BF16
+    same(y, ref.to(BF16), "y")
+
+
+@pytest.mark.parametrize("N,E,k,O,I", [(200, 16, 4, 130, 96), (700, 4, 2, 300, 72), (1500, 4, 2, 1296, 1024),
+                                       (64, 32, 4, 768, 2048)])
+@pytest.mark.parametrize("transposed", [False, True])
+def test_matmul_of_normal_operands(dl, N, E, k, O, I, transposed):
+    print(f"[case] matmul fp8 normal N={N} E={E} k={k} O={O} I={I} t={transposed}", flush=True)
+    gen = _gen(N + O)
+    mask = choose(gen, N, E, k)
+    rows = device_rows(dl, mask, k)
+    inner = O if transposed else I
+    w = dl.do_fp8_pack(torch.randn(E, O, I, generator=gen).cuda(), weights=True)
+    x = dl.do_fp8_pack((torch.randn(N * k, inner, generator=gen) * torch.exp(torch.randn(inner, generator=gen))).cuda())
+    y = dl.do_expert_matmul_fp8(x, w, rows, transposed=transposed)
+    ref, size = _products(values(x), values(w, True), mask, k, transposed, N * k)
+    within(y, ref, product_tol(size, inner, ref, BF16) + eight_bit_tol(size), "y")
+
+
+@pytest.mark.parametrize("R,O,I", [(1, 1, 1), (1, 2048, 768), (5, 33, 7), (130, 256, 128), (1000, 257, 129),
+                                   (2049, 640, 1040)])
+@pytest.mark.parametrize("transposed", [False, True])
+def test_one_matrix_for_all_rows(dl, R, O, I, transposed):
+    print(f"[case] dense fp8 R={R} O={O} I={I} t={transposed}", flush=True)
+    gen = _gen(R + O + I)
+    w = lattice(dl, gen, 1, O, I, weights=True)
+    x = lattice(dl, gen, R, O if transposed else I)
+    y = dl.do_expert_matmul_fp8(x, w, None, transposed=transposed)
+    m = values(w, True)[0]
+    same(y, (values(x) @ (m if transposed else m.t())).to(BF16), "y")
+
+
+@pytest.mark.parametrize("O,I", [(64, 64), (40, 33), (256, 384)])
+@pytest.mark.parametrize("N", [90, 900])
+def test_matmul_rows_past_the_last_are_left(dl, O, I, N):
+    E, k = 4, 4
+    mask = choose(_gen(1), N, E, k)
+    mask[::2, 1:] = False
+    rows = device_rows(dl, mask, k)
+    used = int(rows.offsets[-1])
+    gen = _gen(2)
+    w, x = lattice(dl, gen, E, O, I, weights=True), lattice(dl, gen, N * k, I)
+    x.e[used:] = 255
+    out = torch.full((N * k, O), 7.0, dtype=BF16, device="cuda")
+    print(f"[case] matmul fp8 with {used} of {N * k} rows", flush=True)
+    assert dl.do_expert_matmul_fp8(x, w, rows, out=out) is out
+    ref, _ = _products(values(x), values(w, True), mask, k, False, N * k)
+    same(out[:used], ref[:used].to(BF16), "y")
+    assert (out[used:] == 7.0).all()
+
+
+@pytest.mark.parametrize("N", [20, 300, 3000])
+@pytest.mark.parametrize("shift", [0, 1])
+@pytest.mark.parametrize("transposed", [False, True])
+def test_matmul_alignment(dl, N, shift, transposed):
+    # operands, exponents and output that start one element past a 16-byte boundary; nothing beside the output changes
+    E, k, O, I = 4, 1, 64, 256
+    mask = choose(_gen(3), N, E, k)
+    rows = device_rows(dl, mask, k)
+    inner, outer = (O, I) if transposed else (I, O)
+
+    def moved(a):
+        def one(t, dtype):
+            b = torch.zeros(t.numel() + shift, dtype=torch.uint8, device="cuda")
+            b[shift:] = t.view(torch.uint8).flatten()
+            return b[shift:].view(dtype).view(t.shape)
+        return dl.Fp8(one(a.q, E4M3), one(a.e, torch.uint8))
+
+    gen = _gen(4)
+    w, x = moved(lattice(dl, gen, E, O, I, weights=True)), moved(lattice(dl, gen, N, inner))
+    buf = torch.full((N * outer + 2,), 7.0, dtype=BF16, device="cuda")
+    out = buf[shift:shift + N * outer].view(N, outer)
+    print(f"[case] matmul fp8 shift={shift} N={N} t={transposed}", flush=True)
+    dl.do_expert_matmul_fp8(x, w, rows, transposed=transposed, out=out)
+    ref, _ = _products(values(x), values(w, True), mask, k, transposed, N)
+    same(out, ref.to(BF16), "y")
+    assert (buf[:shift] == 7.0).all() and (buf[shift + N * outer:] == 7.0).all()
+
+
+@pytest.mark.parametrize("N", [30, 500, 3000])
+def test_matmul_blocks_and_values_that_are_nan_stay_in_their_row(dl, N):
+    E, k, O, I = 3, 1, 128, 272
+    mask = choose(_gen(6), N, E, k)
+    rows = device_rows(dl, mask, k)
+    gen = _gen(7)
+    w, x = lattice(dl, gen, E, O, I, weights=True), lattice(dl, gen, N, I)
+    print(f"[case] matmul fp8 NaN N={N}", flush=True)
+    clean = dl.do_expert_matmul_fp8(x, w, rows)
+    x.e[5, 0] = 255                       # a block
+    x.e[11, 2] = 255                      # a row's last, short block
+    x.q.view(torch.uint8)[N - 1, 9] = 0x7F  # one value
+    got = dl.do_expert_matmul_fp8(x, w, rows)
+    hit = torch.zeros(N, dtype=torch.bool, device="cuda")
+    hit[[5, 11, N - 1]] = True
+    assert torch.equal(got[~hit], clean[~hit])
+    assert got[hit].isnan().all()
+
+
+def test_matmul_offsets_and_tokens_out_of_range(dl):
+    # offsets count as the nearest in [0, R], tokens as the nearest in [0, N)
+    N, E, k, O, I = 100, 4, 1, 64, 128
+    gen = _gen(8)
+    w, x = lattice(dl, gen, E, O, I, weights=True), lattice(dl, gen, N, I)
+    off = torch.tensor([-5, 30, 60, 90, 100000], dtype=torch.int32).cuda()
+    tok = torch.arange(N, dtype=torch.int32)
+    tok[3], tok[70] = -7, 1 << 30
+    rows = dl.ExpertRows(off, tok.cuda(), torch.zeros(N, 1, dtype=torch.int32).cuda(),
+                         torch.zeros(N, 1, dtype=torch.int32).cuda())
+    print("[case] matmul fp8 out of range", flush=True)
+    y = dl.do_expert_matmul_fp8(x, w, rows, gather=True)
+    v, m = values(x)[tok.clamp(0, N - 1).long().cuda()], values(w, True)
+    for e, (a, b) in enumerate([(0, 30), (30, 60), (60, 90), (90, 100)]):
+        same(y[a:b], (v[a:b] @ m[e].t()).to(BF16), "y")
+
+
+def test_matmul_far_tokens(dl):
+    # rows taken from tokens more than 4 GiB apart, and a result past 2^31 elements' place
+    N, H, E, O = (1 << 21) + 64, 2048, 2, 64
+    gen = _gen(9)
+    q = torch.zeros(N, H, dtype=torch.uint8, device="cuda").view(E4M3)
+    e = torch.full((N, H // BLOCK), 127, dtype=torch.uint8, device="cuda")
+    part = lattice(dl, gen, 300, H)
+    at = torch.randint(0, N, (300,), generator=gen)
+    at[:4] = torch.tensor([0, N - 1, N - 2, 1 << 21])
+    at = at.unique()
+    n = at.numel()
+    q.view(torch.uint8)[at.cuda()] = part.q.view(torch.uint8)[:n]
+    e[at.cuda()] = part.e[:n]
+    w = lattice(dl, gen, E, O, H, weights=True)
+    tok = torch.zeros(N, dtype=torch.int32)
+    tok[:n] = at.flip(0).int()
+    rows = dl.ExpertRows(torch.tensor([0, 100, n], dtype=torch.int32).cuda(), tok.cuda(),
+                         torch.zeros(N, 1, dtype=torch.int32).cuda(), torch.zeros(N, 1, dtype=torch.int32).cuda())
+    print("[case] matmul fp8 far tokens", flush=True)
+    y = dl.do_expert_matmul_fp8(dl.Fp8(q, e), w, rows, gather=True)
+    v = values(dl.Fp8(part.q[:n], part.e[:n])).flip(0)
+    m = values(w, True)
+    ref = torch.cat([v[:100] @ m[0].t(), v[100:] @ m[1].t()])
+    same(y[:n], ref.to(BF16), "y")
+
+
+# --- the gated activation --------------------------------------------------------------------------------------------
+
+# N, E, k, H, F
+GATED = [(1, 8, 2, 64, 32), (1, 128, 8, 72, 96), (5, 4, 1, 1, 1), (60, 8, 2, 40, 33), (200, 16, 4, 128, 96),
+         (700, 4, 2, 144, 256), (700, 4, 2, 64, 200), (1000, 3, 2, 129, 129), (600, 3, 2, 80, 48), (64, 64, 8, 96, 160),
+         (300, 4, 2, 656, 400), (900, 3, 2, 1040, 272), (130, 4, 2, 333, 64)]
+
+
+def _row_probs(p, mask, k, R):
+    out = torch.zeros(R, dtype=torch.float64, device="cuda")
+    for e, lo, hi, tok in spans(mask, k):
+        out[lo:hi] = 1.0 if p is None else p[tok, e].double()
+    return out[:, None]
+
+
+def _scale(H):
+    """A power of two that leaves a sum of H lattice products (each about 20 in size) at a few units."""
+    return -3 - (max(1, H).bit_length() + 1) // 2
+
+
+def _act8_ref(a):
+    """(q, e) of a [..., W] as the checkpoint holds it."""
+    W = a.shape[-1]
+    v = torch.nn.functional.pad(a, (0, -W % 32)).unflatten(-1, (-1, 32))
+    top = v.abs().amax(-1)
+    m, ex = torch.frexp(top)
+    e = torch.where(top > 0, ex - 7 + (m > 127 / 128).int(), torch.full_like(ex, -126)).clamp(min=-126)
+    q = torch.round(v * power(-e[..., None]))
+    return q.flatten(-2)[..., :W], e
+
+
+def _gated(dl, gen, N, E, k, H, F, dist, pdtype):
+    mask = choose(gen, N, E, k, dist)
+    x, w1 = lattice(dl, gen, N, H, scale=_scale(H)), lattice(dl, gen, E, 2 * F, H, weights=True)
+    p = None if pdtype is None else torch.rand(N, E, generator=gen).to(pdtype).cuda()
+    return mask, device_rows(dl, mask, k), x, w1, p
+
+
+@pytest.mark.parametrize("N,E,k,H,F", GATED)
+@pytest.mark.parametrize("pdtype", [F32, BF16, None])
+@pytest.mark.parametrize("dist", ["even", "idle"])
+def test_swiglu(dl, N, E, k, H, F, pdtype, dist):
+    print(f"[case] swiglu fp8 N={N} E={E} k={k} H={H} F={F} p={pdtype} {dist}", flush=True)
+    mask, rows, x, w1, p = _gated(dl, _gen(H + F), N, E, k, H, F, dist, pdtype)
+    R = N * k
+    h, none = dl.do_expert_swiglu_fp8(x, w1, rows, p)
+    h2, kept = dl.do_expert_swiglu_fp8(x, w1, rows, p, checkpoint=True)
+    assert none is None and torch.equal(h.q.view(torch.uint8), h2.q.view(torch.uint8)) and torch.equal(h.e, h2.e)
+    a, _ = _products(values(x)[rows.row_token.long()], values(w1, True), mask, k, False, R)
+    # the sums are exact, so the checkpoint is too
+    q, e = _act8_ref(a.view(R, 2, F))
+    same(kept.e.int() - 127, e, "checkpoint's exponents")
+    same(kept.q.double(), q, "checkpoint")
+    g, u = a[:, :F], a[:, F:]
+    ref = _row_probs(p, mask, k, R) * g * torch.sigmoid(g) * u
+    err = ref.abs() * (g.abs() + 8) * 4 * EPS32  # exp, the quotient and the products
+    f = power(h.e.int() - 127)
+    pad = torch.nn.functional.pad(ref.abs(), (0, -F % BLOCK)).unflatten(1, (-1, BLOCK))
+    top = pad.amax(2)
+    dtop = torch.nn.functional.pad(err, (0, -F % BLOCK)).unflatten(1, (-1, BLOCK)).amax(2)
+    assert (top <= 448 * f + dtop).all()
+    assert ((top + dtop > 224 * f) | (h.e == 7)).all()
+    # half a step at the value: 2^-4 of its power of two, half of 2^-9 2^e at least
+    wide = spread(f, ref.shape, False)
+    step = power(torch.frexp(ref.abs() + err)[1] - 1)
+    within(values(h), ref, err + torch.maximum(step * 2.0 ** -4, TINY * wide), "h")
+
+
+@pytest.mark.parametrize("N,E,k,H,F", GATED)
+@pytest.mark.parametrize("pdtype", [F32, BF16, None])
+@pytest.mark.parametrize("dist", ["even", "idle"])
+def test_swiglu_grad(dl, N, E, k, H, F, pdtype, dist):
+    print(f"[case] swiglu grad fp8 N={N} E={E} k={k} H={H} F={F} p={pdtype} {dist}", flush=True)
+    gen = _gen(H + F + 1)
+    mask = choose(gen, N, E, k, dist)
+    rows = device_rows(dl, mask, k)
+    R = N * k
+    dy, w2 = lattice(dl, gen, N, H, scale=_scale(H)), lattice(dl, gen, E, H, F, weights=True)
+    p = None if pdtype is None else torch.rand(N, E, generator=gen).to(pdtype).cuda()
+    kept = dl.Act8(torch.randint(-127, 128, (R, 2, F), generator=gen, dtype=torch.int8).cuda(),
+                   torch.randint(118, 124, (R, 2, -(-F // 32)), generator=gen, dtype=torch.uint8).cuda())
+    da, h, dp = dl.do_expert_swiglu_grad_fp8(dy, w2, rows, kept, p)
+    assert da.dtype == h.dtype == BF16
+    scale = power(kept.e.int() - 127)
+    a = kept.q.double() * scale.repeat_interleave(32, 2)[..., :F]
+    g, u = a[:, 0], a[:, 1]
+    pr = _row_probs(p, mask, k, R)
+    dh, _ = _products(values(dy)[rows.row_token.long()], values(w2, True), mask, k, True, R)  # exact
+    z = torch.sigmoid(g)
+    s, slope = g * z * u, z * (1 + g * (1 - z))
+    fn = (g.abs() + 8) * 4 * EPS32  # exp and the quotient, relative to z
+
+    def close(got, ref, tol, what):
+        within(got, ref, tol + EPS16 * (ref.abs() + tol) + 1e-30, what)
+
+    close(h, pr * s, (pr * s).abs() * fn, "h")
+    rg, ru = pr * dh * u * slope, pr * dh * g * z
+    # the slope's terms z and g z (1 - z) carry the error of z each
+    close(da[:, :F], rg, pr * (dh * u).abs() * (z + 2 * g.abs() * z) * fn + rg.abs() * 8 * EPS32, "dg")
+    close(da[:, F:], ru, ru.abs() * (fn + 8 * EPS32), "du")
+    if p is None:
+        assert dp is None
+        return
+    assert dp.dtype == p.dtype
+    ref = torch.zeros(N, E, dtype=torch.float64, device="cuda")
+    tol = torch.zeros_like(ref)
+    for e, lo, hi, tok in spans(mask, k):
+        ref[tok, e] = (dh * s)[lo:hi].sum(1)
+        tol[tok, e] = ((dh * s).abs() * (fn + 4 * (F + 4) * EPS32))[lo:hi].sum(1)
+    assert not dp[~mask.cuda()].any()
+    within(dp, ref, tol + (EPS16 if pdtype == BF16 else EPS32) * (ref.abs() + tol) + 1e-30, "dp")
+
+
+def test_swiglu_grad_against_differences(dl):
+    # sum(dy * y) of y_t = sum_e p_te W2_e (silu(g) u): central differences in 64 bits along directions of p, g and u
+    N, E, k, H, F = 40, 6, 2, 24, 48
+    gen = _gen(11)
+    mask = choose(gen, N, E, k)
+    rows = device_rows(dl, mask, k)
+    R = N * k
+    dy, w2 = lattice(dl, gen, N, H, scale=_scale(H)), lattice(dl, gen, E, H, F, weights=True)
+    p = torch.rand(N, E, generator=gen).cuda()
+    kept = dl.do_act8_pack(torch.randn(R, 2, F, generator=gen).cuda())
+    da, _, dp = dl.do_expert_swiglu_grad_fp8(dy, w2, rows, kept, p)
+    a = dl.do_act8_unpack(kept, F32).double().view(R, 2 * F)
+    ev = torch.empty(R, dtype=torch.long)
+    for e, lo, hi, _ in spans(mask, k):
+        ev[lo:hi] = e
+    ev, tok = ev.cuda(), rows.row_token.long()
+    dyv, wv = values(dy), values(w2, True)
+
+    def loss(a, p):
+        s = p[tok, ev][:, None] * a[:, :F] * torch.sigmoid(a[:, :F]) * a[:, F:]
+        return (dyv[tok] * torch.bmm(wv[ev], s[:, :, None])[:, :, 0]).sum()
+
+    for seed in range(3):
+        va = torch.randn(R, 2 * F, generator=_gen(seed), dtype=torch.float64).cuda()
+        vp = torch.randn(N, E, generator=_gen(seed + 9), dtype=torch.float64).cuda()
+        t = 1e-4
+        fd = (loss(a + t * va, p.double() + t * vp) - loss(a - t * va, p.double() - t * vp)) / (2 * t)
+        an = (da.double() * va).sum() + (dp.double() * vp).sum()
+        size = (da.double() * va).abs().sum() + (dp.double() * vp).abs().sum()
+        # da is rounded to bf16, EPS16 of every term at most; the difference is off by about t^2
+        assert abs(fd.item() - an.item()) <= (EPS16 + 10 * t * t + 1e-6) * size.item(), (fd.item(), an.item())
+
+
+@pytest.mark.parametrize("N", [20, 200, 1200])
+def test_swiglu_nan_stays_in_its_rows(dl, N):
+    E, k, H, F = 4, 2, 272, 144
+    mask, rows, x, w1, p = _gated(dl, _gen(13), N, E, k, H, F, "even", F32)
+    print(f"[case] swiglu fp8 NaN N={N}", flush=True)
+    clean, kept = dl.do_expert_swiglu_fp8(x, w1, rows, p, checkpoint=True)
+    x.e[7, 1] = 255
+    got, kept2 = dl.do_expert_swiglu_fp8(x, w1, rows, p, checkpoint=True)
+    hit = rows.row_token == 7
+    assert torch.equal(got.q.view(torch.uint8)[~hit], clean.q.view(torch.uint8)[~hit])
+    assert torch.equal(got.e[~hit], clean.e[~hit]) and torch.equal(kept2.q[~hit], kept.q[~hit])
+    assert (got.e[hit] == 255).all() and not got.q.view(torch.uint8)[hit].any()
+    assert (kept2.e[hit] == 255).all() and not kept2.q[hit].any()
+
+
+# --- together --------------------------------------------------------------------------------------------------------
+
+
+def _layer_step(dl, x, dy, w1, w2, rows, p):
+    """Forward and backward of the experts in 8 bits as a training step runs them, weight gradients in bf16."""
+    xq = dl.do_fp8_pack(x)
+    h, kept = dl.do_expert_swiglu_fp8(xq, w1, rows, p, checkpoint=True)
+    y = dl.do_expert_combine(dl.do_expert_matmul_fp8(h, w2, rows), rows)
+    da, again, dp = dl.do_expert_swiglu_grad_fp8(dl.do_fp8_pack(dy), w2, rows, kept, p)
+    dw2 = dl.do_expert_weight_grad(dy, again, rows, gather_dy=True)
+    dw1 = dl.do_expert_weight_grad(da, x, rows, gather_x=True)
+    dx = dl.do_expert_combine(dl.do_expert_matmul_fp8(dl.do_fp8_pack(da), w1, rows, transposed=True), rows)
+    return y, dp, dw1, dw2, dx
+
+
+def _near(got, ref, tol, what):
+    rel = ((got.double() - ref).norm() / ref.norm()).item()
+    assert rel <= tol, (what, rel)
+
+
+@pytest.mark.parametrize("N,E,k,H,F", [(50, 8, 2, 136, 72), (600, 4, 2, 256, 384)])
+def test_a_training_step(dl, N, E, k, H, F):
+    # against the layer in 64 bits with weights as packed.  Each rounding to e4m3 is off by 2^-4 of a value at most, and
+    # so is a sum of values in norm; x, h and, for dx, da and dy, are rounded, with slopes up to 1.1 (silu) and both
+    # factors of a product: 4 roundings' worth bound y, 8 the gradients
+    gen = _gen(N)
+    mask = choose(gen, N, E, k)
+    rows = device_rows(dl, mask, k)
+    x, dy = torch.randn(N, H, generator=gen).bfloat16().cuda(), torch.randn(N, H, generator=gen).bfloat16().cuda()
+    w1 = dl.do_fp8_pack((torch.randn(E, 2 * F, H, generator=gen) * H ** -0.5).cuda(), weights=True)
+    w2 = dl.do_fp8_pack((torch.randn(E, H, F, generator=gen) * F ** -0.5).cuda(), weights=True)
+    p = torch.rand(N, E, generator=gen).cuda()
+    print(f"[case] a step in fp8 N={N}", flush=True)
+    y, dp, dw1, dw2, dx = _layer_step(dl, x, dy, w1, w2, rows, p)
+    xv, pv = x.double().requires_grad_(), p.double().requires_grad_()
+    a1, a2 = values(w1, True).requires_grad_(), values(w2, True).requires_grad_()
+    out = torch.zeros(N, H, dtype=torch.float64, device="cuda")
+    for e, lo, hi, tok in spans(mask, k):
+        a = xv[tok] @ a1[e].t()
+        s = pv[tok, e][:, None] * torch.nn.functional.silu(a[:, :F]) * a[:, F:]
+        out = out.index_add(0, tok, s @ a2[e].t())
+    out.backward(dy.double())
+    _near(y, out.detach(), 4 * 2.0 ** -4, "y")
+    for what, got, ref in (("dp", dp, pv.grad), ("dw1", dw1, a1.grad), ("dw2", dw2, a2.grad), ("dx", dx, xv.grad)):
+        _near(got, ref, 8 * 2.0 ** -4, what)
+
+
+def test_streams_and_replays(dl):
+    # another stream than the default; a captured step replayed on new inputs beside eager calls; two graphs
+    N, E, k, H, F = 300, 4, 2, 256, 160
+    gen = _gen(21)
+    w1 = dl.do_fp8_pack((torch.randn(E, 2 * F, H, generator=gen) * H ** -0.5).cuda(), weights=True)
+    w2 = dl.do_fp8_pack((torch.randn(E, H, F, generator=gen) * F ** -0.5).cuda(), weights=True)
+    inputs = []
+    for i in range(4):
+        mask = choose(gen, N, E, k)
+        inputs.append((torch.randn(N, H, generator=gen).bfloat16().cuda(), torch.randn(N, H, generator=gen).bfloat16().cuda(),
+                       device_rows(dl, mask, k), torch.rand(N, E, generator=gen).cuda()))
+    print("[case] fp8 streams and graphs", flush=True)
+    want = [_layer_step(dl, x, dy, w1, w2, rows, p) for x, dy, rows, p in inputs]
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        x, dy, rows, p = inputs[1]
+        got = _layer_step(dl, x, dy, w1, w2, rows, p)
+    s.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want[1]))
+    x, dy, rows, p = (t.clone() if torch.is_tensor(t) else dl.ExpertRows(*(u.clone() for u in t)) for t in inputs[0])
+    graphs = []
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out = _layer_step(dl, x, dy, w1, w2, rows, p)
+        graphs.append((g, out))
+    for i in (2, 0, 3, 1):
+        for dst, src in zip((x, dy, *rows, p), (*inputs[i][:2], *inputs[i][2], inputs[i][3])):
+            dst.copy_(src)
+        for g, out in graphs:
+            g.replay()
+        eager = _layer_step(dl, x, dy, w1, w2, rows, p)
+        torch.cuda.synchronize()
+        for a, b, c, d in zip(graphs[0][1], graphs[1][1], eager, want[i]):
+            assert torch.equal(a, d) and torch.equal(b, d) and torch.equal(c, d)
+
+
+def test_calls_do_not_depend_on_what_ran_before(dl):
+    # the same call twice with others of other sizes between
+    gen = _gen(31)
+    N, E, k, O, I = 257, 8, 2, 272, 528
+    mask = choose(gen, N, E, k)
+    rows = device_rows(dl, mask, k)
+    w, x = lattice(dl, gen, E, O, I, weights=True), lattice(dl, gen, N * k, I)
+    first = dl.do_expert_matmul_fp8(x, w, rows)
+    for n in (1, 1000):
+        dl.do_expert_matmul_fp8(lattice(dl, gen, n, 128), lattice(dl, gen, 1, 64, 128, weights=True), None)
+    assert torch.equal(dl.do_expert_matmul_fp8(x, w, rows), first)
+    assert blocks(I) == x.e.shape[1]
