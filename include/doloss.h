@@ -527,6 +527,28 @@ do_status do_expert_swiglu_grad_fp8(const uint8_t* dy, const uint8_t* dy_exp, co
                                     int64_t workspace_bytes, hipStream_t stream);
 
 /*
+ * The whole layer of a few tokens, N <= 64, as in a serving step: y_t = sum
+ * over t's k best experts of p_te W2_e (silu(g) u), (g, u) = W1_e x_t, from
+ * the router's scores (ranked as by do_topk_signature) to the outputs.
+ *   x       [N][H] device of dtype;  y  [N][H] device of dtype, overwritten
+ *   scores  [N][E] device of scores_dtype
+ *   p       nullable, [N][E] device of p_dtype: routing probabilities
+ *   w1      [E][2 F][H], w2 [E][H][F] device, of dtype; or, with w1_exp and
+ *           w2_exp, in 8-bit floating point (do_fp8_pack_weights)
+ *   workspace  device, 16-byte aligned, do_expert_layer_workspace(..) bytes at
+ *           least (0 for arguments that are refused); no two calls that may
+ *           overlap in time share one
+ * Products, sums and activations are computed in fp32, the activations between
+ * the products rounded to dtype; a token's sum is taken in an order that the
+ * call's sizes and choices fix.
+ */
+int64_t do_expert_layer_workspace(do_dtype dtype, int64_t N, int32_t E, int32_t k, int32_t F);
+do_status do_expert_layer(const void* x, do_dtype dtype, const void* scores, do_dtype scores_dtype, const void* p,
+                          do_dtype p_dtype, const void* w1, const uint8_t* w1_exp, const void* w2,
+                          const uint8_t* w2_exp, int64_t N, int32_t E, int32_t k, int32_t H, int32_t F, void* y,
+                          void* workspace, int64_t workspace_bytes, hipStream_t stream);
+
+/*
  * Process-wide options (they take effect at the next call; calls already
  * enqueued are unaffected).  Returns DO_ERR_INVALID_ARG for an unknown option
  * or a value out of range.  The first two override internal choices that

@@ -20,6 +20,7 @@ Functions keep the C names:
 * ``do_act8_pack`` / ``do_act8_unpack`` -> activations in 8 bits (Act8) and back
 * ``do_fp8_pack`` / ``do_fp8_unpack`` -> rows or weights in 8-bit floating point (Fp8) and back, and the experts'
   products on them: ``do_expert_swiglu_fp8`` / ``do_expert_swiglu_grad_fp8``, ``do_expert_matmul_fp8``
+* ``do_expert_layer`` -> the whole layer of up to 64 tokens, from their scores to their outputs
 
 ``scores`` is a CUDA tensor of shape [N, E] or [L, N, E], float32 or bfloat16.
 """
@@ -103,6 +104,8 @@ def lib():
                                      st),
             "do_expert_swiglu_grad_fp8": ([vp, vp, vp, vp, vp, st, vp, vp, vp, vp, i64, i32, i32, i32, i32, vp, vp, vp,
                                            vp, vp, vp, i64, vp], st),
+            "do_expert_layer_workspace": ([st, i64, i32, i32, i32], i64),
+            "do_expert_layer": ([vp, st, vp, st, vp, st, vp, vp, vp, vp, i64, i32, i32, i32, i32, vp, vp, i64, vp], st),
             "do_rem_allocate": ([vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp, vp], st),
             "do_rem_dispatch": ([vp, vp, i32, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp, vp], st),
         }
@@ -939,3 +942,45 @@ def do_expert_swiglu_grad_fp8(dy: Fp8, w2: Fp8, rows: ExpertRows, checkpoint: Ac
                                            ws.data_ptr() if ws is not None else None, need, _stream()),
            "do_expert_swiglu_grad_fp8")
     return da, h, dp
+
+
+LAYER_TOKENS = 64
+
+
+def do_expert_layer(x: torch.Tensor, scores: torch.Tensor, k: int, w1, w2, p: torch.Tensor | None = None,
+                    out: torch.Tensor | None = None) -> torch.Tensor:
+    """y [N, H]: the experts' layer of up to 64 tokens x [N, H], y_t = sum over the k highest scores [N, E] of
+    p_te W2_e (silu(g) u), (g, u) = W1_e x_t.  w1 [E, 2 F, H] and w2 [E, H, F] are of x's type, or both Fp8
+    (do_fp8_pack with weights=True); p [N, E] or None (1)."""
+    if not isinstance(x, torch.Tensor) or x.dim() != 2 or not 1 <= x.shape[0] <= LAYER_TOKENS:
+        raise ValueError(f"x must be a tensor of shape [N, H] with 1 to {LAYER_TOKENS} tokens")
+    _want(x, "x", dtypes=_SCORE_DTYPES)
+    N, H = x.shape
+    if not isinstance(scores, torch.Tensor) or scores.dim() != 2 or scores.shape[0] != N:
+        raise ValueError(f"scores must be a tensor of shape [{N}, E]")
+    _want(scores, "scores", dtypes=_SCORE_DTYPES)
+    E = scores.shape[1]
+    if not 1 <= k <= E:
+        raise ValueError(f"k = {k} must be in [1, E = {E}]")
+    if isinstance(w1, Fp8) != isinstance(w2, Fp8):
+        raise ValueError("w1 and w2 must both be Fp8 or both tensors")
+    if isinstance(w1, Fp8):
+        F2, _ = _fp8_weights(w1, "w1", E)
+        F = F2 // 2
+        _want_fp8(w1, "w1", (E, 2 * F, H), True)
+        _want_fp8(w2, "w2", (E, H, F), True)
+        ptrs = (w1.q.data_ptr(), w1.e.data_ptr(), w2.q.data_ptr(), w2.e.data_ptr())
+    else:
+        if not isinstance(w1, torch.Tensor) or w1.dim() != 3:
+            raise ValueError(f"w1 must be a tensor of shape [{E}, 2 F, {H}]")
+        F = w1.shape[1] // 2
+        _operand(w1, "w1", (E, 2 * F, H), x)
+        _operand(w2, "w2", (E, H, F), x)
+        ptrs = (w1.data_ptr(), None, w2.data_ptr(), None)
+    pp, pd = _probs_of(p, N, E)
+    y = _out(out, "out", (N, H), x.dtype, x.device)
+    need = lib().do_expert_layer_workspace(_dtype_code(x), N, E, k, F)
+    ws = torch.empty(need, dtype=torch.uint8, device=x.device)
+    _check(lib().do_expert_layer(x.data_ptr(), _dtype_code(x), scores.data_ptr(), _dtype_code(scores), pp, pd, *ptrs, N,
+                                 E, k, H, F, y.data_ptr(), ws.data_ptr(), need, _stream()), "do_expert_layer")
+    return y

@@ -514,3 +514,56 @@ DOLOSS_API do_status do_expert_swiglu_grad_fp8(const uint8_t* dy, const uint8_t*
   return launched(
       dol::launch_expert_dp(g.dp, (F + 63) / 64, g.R, token_row, token_expert, N, k, E, dp, p_dtype, stream));
 }
+
+// ---- the layer of a few tokens --------------------------------------------------
+
+DOLOSS_API int64_t do_expert_layer_workspace(do_dtype dtype, int64_t N, int32_t E, int32_t k, int32_t F) {
+  if ((dtype != DO_F32 && dtype != DO_BF16) || N < 1 || N > dol::kLayerTokens || E < 1 || E > dol::kMaxE || k < 1 ||
+      k > E || F < 1 || F > dol::kMaxWidth)
+    return 0;
+  return dol::expert_layer_bytes(dtype, N, E, k, F);
+}
+
+DOLOSS_API do_status do_expert_layer(const void* x, do_dtype dtype, const void* scores, do_dtype scores_dtype,
+                                     const void* p, do_dtype p_dtype, const void* w1, const uint8_t* w1_exp,
+                                     const void* w2, const uint8_t* w2_exp, int64_t N, int32_t E, int32_t k, int32_t H,
+                                     int32_t F, void* y, void* workspace, int64_t workspace_bytes,
+                                     hipStream_t stream) {
+  DO_TRY(check_dtype(dtype));
+  DO_TRY(check_dtype(scores_dtype));
+  DO_TRY(check_experts(N, E, k));
+  DO_TRY(check_widths(N, E, {H, F}));
+  if (N > dol::kLayerTokens) return set_error(DO_ERR_INVALID_ARG, "N must be in [1, 64]");
+  if ((w1_exp == nullptr) != (w2_exp == nullptr))
+    return set_error(DO_ERR_INVALID_ARG, "both weights are in 8 bits or neither is");
+  const size_t w_size = w1_exp != nullptr ? 1 : size_of(dtype);
+  DO_TRY(check_ptr(x, size_of(dtype), "x is NULL or not aligned to its element size"));
+  DO_TRY(check_ptr(scores, size_of(scores_dtype), "scores is NULL or not aligned to its element size"));
+  DO_TRY(check_ptr(w1, w_size, "w1 is NULL or not aligned to its element size"));
+  DO_TRY(check_ptr(w2, w_size, "w2 is NULL or not aligned to its element size"));
+  DO_TRY(check_ptr(y, size_of(dtype), "y is NULL or not aligned to its element size"));
+  if (p != nullptr) {
+    DO_TRY(check_dtype(p_dtype));
+    if (!aligned(p, size_of(p_dtype))) return set_error(DO_ERR_INVALID_ARG, "p is not aligned to its element size");
+  }
+  DO_TRY(check_ptr(workspace, 16, "workspace is NULL or not 16-byte aligned"));
+  if (workspace_bytes < do_expert_layer_workspace(dtype, N, E, k, F))
+    return set_error(DO_ERR_INVALID_ARG, "workspace is smaller than do_expert_layer_workspace(dtype, N, E, k, F)");
+  dol::LayerArgs a{};
+  a.x = x;
+  a.scores = scores;
+  a.scores_bf16 = scores_dtype == DO_BF16;
+  a.p = p;
+  a.p_bf16 = p_dtype == DO_BF16;
+  a.w1 = w1;
+  a.w1_exp = w1_exp;
+  a.w2 = w2;
+  a.w2_exp = w2_exp;
+  a.y = y;
+  a.N = (int32_t)N;
+  a.E = E;
+  a.k = k;
+  a.H = H;
+  a.F = F;
+  return launched(dol::launch_expert_layer(a, dtype, workspace, stream));
+}

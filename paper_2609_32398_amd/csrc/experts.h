@@ -83,6 +83,33 @@ hipError_t launch_expert_dp(const float* part, int32_t nparts, int64_t R, const 
                             const int32_t* token_expert, int64_t N, int32_t k, int32_t E, void* dp, do_dtype dt,
                             hipStream_t s);
 
+// The layer of a few tokens: a chosen expert, its first row and its tokens (bit t: token t).
+struct Chosen {
+  int32_t e, first;
+  u64 tokens;
+};
+constexpr int kLayerTokens = 64;
+struct LayerArgs {
+  const void* x;          // [N][H]
+  const void* scores;     // [N][E]
+  const void* p;          // nullable [N][E]
+  const void* w1;         // [E][2 F][H] and its exponents (8 bits)
+  const void* w2;         // [E][H][F]
+  const uint8_t* w1_exp;
+  const uint8_t* w2_exp;
+  void* y;                // [N][H]
+  int32_t* n_chosen;      // workspace
+  Chosen* chosen;
+  void* h;                // activations, rows by expert
+  int32_t N, E, k, H, F;
+  int32_t ldh;            // elements of a row of h
+  int32_t scores_bf16, p_bf16;
+};
+// Rows of the activations are whole 16-byte pieces.
+inline int32_t layer_row(do_dtype dt, int32_t F) { return dt == DO_F32 ? (F + 3) & ~3 : (F + 7) & ~7; }
+int64_t expert_layer_bytes(do_dtype dt, int64_t N, int32_t E, int32_t k, int32_t F);
+hipError_t launch_expert_layer(LayerArgs a, do_dtype dt, void* workspace, hipStream_t s);
+
 // ---- bf16 and 8-bit conversions ---------------------------------------------
 
 __device__ __forceinline__ float bf16_float(uint16_t b) { return __uint_as_float((uint32_t)b << 16); }

@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "libdoloss.so")
 SOURCES = ["api.hip", "topk.hip", "topk_ragged.hip", "topk_pieces.hip", "topk_wide.hip", "reduce.hip", "surrogate.hip", "loadstats.hip", "rem.hip",
            "expert_api.hip", "expert_rows.hip", "expert_matmul_bf16.hip", "expert_matmul_f32.hip", "expert_wgrad_bf16.hip", "expert_wgrad_f32.hip", "expert_swiglu.hip", "expert_skinny.hip", "act8.hip",
-           "fp8.hip", "expert_matmul_fp8.hip", "expert_swiglu_fp8.hip"]
+           "fp8.hip", "expert_matmul_fp8.hip", "expert_swiglu_fp8.hip", "expert_layer.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950",

@@ -52,6 +52,23 @@ def test_products(dl):
         (21, 79, 1)])
 
 
+def test_layer(dl):
+    L = dl.lib()
+    need = L.do_expert_layer_workspace(1, 10, 8, 2, 60)
+    assert need == 16 + 8 * 16 + 20 * 64 * 2
+    assert L.do_expert_layer_workspace(0, 1, 8, 2, 61) == 16 + 2 * 16 + 2 * 64 * 4
+    for bad in ((2, 10, 8, 2, 60), (1, 0, 8, 2, 60), (1, 65, 8, 2, 60), (1, 10, 0, 1, 60), (1, 10, 1025, 2, 60),
+                (1, 10, 8, 0, 60), (1, 10, 8, 9, 60), (1, 10, 8, 2, 0), (1, 10, 8, 2, 65537)):
+        assert L.do_expert_layer_workspace(*bad) == 0
+    _rejects(dl, "do_expert_layer",
+             [FAKE, 1, FAKE, 0, FAKE, 0, FAKE, FAKE, FAKE, FAKE, 10, 8, 2, 64, 60, FAKE, FAKE, need, None], [
+                 (0, None, 1), (0, FAKE + 1, 1), (1, 2, 2), (2, None, 1), (2, FAKE + 2, 1), (3, 2, 2), (4, FAKE + 2, 1),
+                 (5, 2, 2), (6, None, 1), (7, None, 1), (8, None, 1), (9, None, 1), (10, 0, 1), (10, 65, 1), (11, 0, 1),
+                 (11, 1025, 1), (12, 0, 1), (12, 9, 1), (13, 0, 1), (13, 65537, 1), (14, 0, 1), (14, 65537, 1),
+                 (15, None, 1), (15, FAKE + 1, 1), (16, None, 1), (16, FAKE + 8, 1), (17, need - 1, 1),
+                 ((6, 7, 9), (FAKE + 1, None, None), 1)])
+
+
 def _fp8(dl, *shape, e=None, dtype=E4M3):
     return dl.Fp8(torch.zeros(shape, dtype=dtype), torch.zeros(e or (*shape[:-1], -(-shape[-1] // 128)), dtype=torch.uint8))
 
@@ -79,5 +96,9 @@ def test_binding(dl):
     _refused(dl.do_expert_matmul_fp8, _fp8(dl, 10, 64), _fp8(dl, 2, 32, 64, e=(2, 1, 1)), None, say="[1, O, I]")
     _refused(dl.do_expert_matmul_fp8, torch.zeros(10, 64), _fp8(dl, 1, 32, 64, e=(1, 1, 1)), None)
     _refused(dl.do_expert_matmul_fp8, _fp8(dl, 20, 64), _fp8(dl, 4, 32, 64, e=(4, 1, 1)), "rows", say="ExpertRows")
+    w1, w2 = torch.zeros(4, 16, 64), torch.zeros(4, 64, 8)
+    _refused(dl.do_expert_layer, torch.zeros(65, 64), torch.zeros(65, 4), 2, w1, w2, say="1 to 64 tokens")
+    _refused(dl.do_expert_layer, torch.zeros(0, 64), torch.zeros(0, 4), 2, w1, w2, say="1 to 64 tokens")
+    _refused(dl.do_expert_layer, torch.zeros(2, 64), torch.zeros(2, 4), 2, w1, w2, say="device tensor")
     _refused(dl.do_expert_swiglu_fp8, _fp8(dl, 10, 64), torch.zeros(4, 32, 64), rows)
     _refused(dl.do_expert_swiglu_grad_fp8, _fp8(dl, 10, 64), torch.zeros(4, 64, 32), rows, None)
