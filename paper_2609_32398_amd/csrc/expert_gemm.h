@@ -143,6 +143,11 @@ __device__ __forceinline__ void word_to_lds(const void* src, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(src));
 }
 
+// One byte per lane to a word per lane.
+__device__ __forceinline__ void byte_to_lds(const void* src, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_ubyte %1, off" ::"s"(lds), "v"(src));
+}
+
 // All but the last `newest` of this wave's loads and stores are done (they are
 // counted in order).
 template <int newest>
@@ -761,15 +766,20 @@ constexpr int kLists = EPI == kWeightGrad ? (GP ? 2 : 0) + (GQ ? 2 : 0) : 0;
 template <typename C, int EPI>
 constexpr int kProbs = EPI == kSwiglu || EPI == kSwigluGrad ? C::BQ : 0;
 
+// A stage in LDS: the operands' pieces, and in 8 bits a word for each operand row's exponent.
+template <typename T, typename C>
+constexpr int kStage = C::stage + (sizeof(T) == 1 ? 4 * (C::BP + (C::BQ < kWave ? kWave : C::BQ)) : 0);
+
 template <typename T, typename C, int LP, int LQ, int EPI, int LOAD, bool GP, bool GQ>
 __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const ExpertGemm g) {
   extern __shared__ __align__(16) char sm[];  // two stages, token lists, row probabilities, the tile list
   constexpr int KS = kStageBytes / (int)sizeof(T);
   constexpr int BPo = EPI == kSwiglu ? C::BP / 2 : C::BP;  // output columns of a tile
   constexpr bool F8 = sizeof(T) == 1;
+  constexpr int STAGE = kStage<T, C>;
   using OT = Stored<T>;
-  int32_t* first = reinterpret_cast<int32_t*>(sm + 2 * C::stage);  // [E + 1] first tile of an expert
-  int32_t* lists = reinterpret_cast<int32_t*>(sm + 2 * C::stage);  // of tokens, two for each gathered operand
+  int32_t* first = reinterpret_cast<int32_t*>(sm + 2 * STAGE);  // [E + 1] first tile of an expert
+  int32_t* lists = reinterpret_cast<int32_t*>(sm + 2 * STAGE);  // of tokens, two for each gathered operand
   first += kLists<EPI, GP, GQ> * kList;
   float* probs = reinterpret_cast<float*>(first);  // of a tile's rows
   first += kProbs<C, EPI>;
@@ -866,8 +876,10 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
     }
   }
   // the tokens of a thread's rows of a tile, loaded ahead of start()
+  constexpr int NPE = F8 ? C::BP / C::loaders : 1, NQE = F8 ? (C::BQ + C::loaders - 1) / C::loaders : 1;
+  static_assert(!F8 || C::BP % C::loaders == 0);
   struct Tokens {
-    int32_t t[LoaderQ::N];
+    int32_t t[LoaderQ::N], of_exp[NQE];
   };
   auto tokens = [&](const Where& w) {
     Tokens k;
@@ -875,6 +887,10 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
 #pragma unroll
       for (int j = 0; j < LoaderQ::N; ++j)
         k.t[j] = g.q_token[w.r0 + min(LoaderQ::row(tid) + j * LoaderQ::RS, w.rows - 1)];
+      if constexpr (F8) {
+#pragma unroll
+        for (int j = 0; j < NQE; ++j) k.of_exp[j] = g.q_token[w.r0 + min(tid + j * C::loaders, w.rows - 1)];
+      }
     }
     return k;
   };
@@ -885,7 +901,31 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
     return EPI == kSwiglu ? (i >> 6) * 32 + (i & 31) : i;
   };
   auto up_p = [](int j) { return EPI == kSwiglu ? (j * LoaderP::RS >> 5) & 1 : 0; };
+  // 8 bits: the exponents of operand rows tid, tid + loaders, .. of the tile, a byte for each stage
+  const int lrow = lane & 31;
+  const uint8_t *pexp[NPE], *qexp[NQE];
+  const int64_t KB = (g.K + KS - 1) / KS, pexp_step = LP == kInner ? 1 : (g.Pd + KS - 1) / KS;
+  auto start_exponents = [&](const Where& w, const Tokens& k) {
+#pragma unroll
+    for (int j = 0; j < NPE; ++j) {
+      const int i = tid + j * C::loaders;
+      if constexpr (LP == kInner) {
+        const int64_t PB = ((EPI == kSwiglu ? 2 : 1) * (int64_t)g.Pd + KS - 1) / KS;
+        const int64_t row = EPI == kSwiglu ? min(w.p0 + (i >> 6) * 32 + (i & 31), g.Pd - 1) + (i >> 5 & 1) * (int64_t)g.Pd
+                                           : min(w.p0 + i, g.Pd - 1);
+        pexp[j] = g.p_exp + (w.e * PB + row / KS) * KB;
+      } else {
+        pexp[j] = g.p_exp + w.e * KB * pexp_step + min(w.p0 + i, g.Pd - 1) / KS;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < NQE; ++j) {
+      const int i = min(tid + j * C::loaders, w.rows - 1);
+      qexp[j] = g.q_exp + (GQ ? clip_token(k.of_exp[j], (int32_t)(g.N - 1)) : w.r0 + i) * KB;
+    }
+  };
   auto start = [&](const Where& w, const Tokens& k) {
+    if constexpr (F8) start_exponents(w, k);
     const T* P = static_cast<const T*>(g.P);
     const T* Q = static_cast<const T*>(g.Q);
     if constexpr (EPI == kWeightGrad) {
@@ -916,7 +956,8 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
       }
     }
   };
-  const uint32_t wave_lds = (uint32_t)(uintptr_t)(DOL_LDS char*)sm + (uint32_t)(tid & ~63) * 16;
+  const uint32_t lds_base = (uint32_t)(uintptr_t)(DOL_LDS char*)sm;
+  const uint32_t wave_lds = lds_base + (uint32_t)(tid & ~63) * 16;
 
   // The loaders run a stage ahead of the products, through the tiles in the same order.
   const bool loader = tid < C::loaders;
@@ -948,7 +989,7 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
   constexpr int kLoads = LoaderP::N + LoaderQ::N;
   auto load = [&](auto which) {
     constexpr int I = decltype(which)::value;
-    const int at = load_slot * C::stage + (I < LoaderP::N ? 0 : C::BP * kStageBytes);
+    const int at = load_slot * STAGE + (I < LoaderP::N ? 0 : C::BP * kStageBytes);
     auto one = [&](auto& l, auto piece) {
       constexpr int j = decltype(piece)::value;
       if constexpr (!VEC) {
@@ -968,11 +1009,26 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
     else
       one(lq, std::integral_constant<int, I - LoaderP::N>{});
   };
+  auto load_exponents = [&] {
+    const uint32_t dst = lds_base + load_slot * STAGE + C::stage + (tid & ~63) * 4;
+#pragma unroll
+    for (int j = 0; j < NPE; ++j) {
+      byte_to_lds(pexp[j], __builtin_amdgcn_readfirstlane(dst + j * C::loaders * 4));
+      pexp[j] += pexp_step;
+    }
+#pragma unroll
+    for (int j = 0; j < NQE; ++j) {
+      if (tid - lane + j * C::loaders < C::BQ)
+        byte_to_lds(qexp[j], __builtin_amdgcn_readfirstlane(dst + (C::BP + j * C::loaders) * 4));
+      ++qexp[j];
+    }
+  };
   auto load_stage = [&] {
     if (!loading) return;
+    if constexpr (F8) load_exponents();
     if constexpr (!VEC && kLoads <= 12) {
       v4u vp[LoaderP::N], vq[LoaderQ::N];
-      char* st = sm + load_slot * C::stage;
+      char* st = sm + load_slot * STAGE;
       lp.template fetch<0, LoaderP::N>(vp);
       lq.template fetch<0, LoaderQ::N>(vq);
       lp.template put<0, LoaderP::N>(tid, st, vp);
@@ -1000,90 +1056,32 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
   auto clear = [&](int b) {
     if constexpr (VEC) {
       if (have < KS) {
-        LoaderP::clear(tid, have, sm + b * C::stage);
-        LoaderQ::clear(tid, have, sm + b * C::stage + C::BP * kStageBytes);
+        LoaderP::clear(tid, have, sm + b * STAGE);
+        LoaderQ::clear(tid, have, sm + b * STAGE + C::BP * kStageBytes);
       }
     }
-  };
-
-  // 8 bits: the operands' exponents, four stages of a lane's rows at a time, the next stage's in the low byte.
-  constexpr int NP = LP == kInner ? C::MP : 4;  // k outer: a byte for each of the four stages
-  struct Exponents {
-    uint32_t p[F8 ? NP : 1], q[F8 ? C::MQ : 1];
-  };
-  struct RowsOf {
-    int32_t r[F8 ? C::MQ : 1];
-  };
-  const int lrow = lane & 31;
-  // a lane's rows of a tile, the tokens' where they are taken by token
-  auto rows_at = [&](const Where& w) {
-    RowsOf k{};
-    if constexpr (F8) {
-#pragma unroll
-      for (int j = 0; j < C::MQ; ++j) {
-        const int r = w.r0 + min(wq * (C::BQ / C::WQ) + j * 32 + lrow, w.rows - 1);
-        k.r[j] = GQ ? g.q_token[r] : r;
-      }
-    }
-    return k;
-  };
-  // four bytes from place i of an array of n, as far as there are some
-  auto four = [](const uint8_t* a, int64_t i, int64_t n) {
-    if (n >= 4) {
-      const int64_t at = i < n - 4 ? i : n - 4;
-      uint32_t v;
-      __builtin_memcpy(&v, a + at, 4);
-      return v >> (8 * (int)(i - at));
-    }
-    uint32_t v = 0;
-    for (int b = 0; b < 3; ++b)
-      if (i + b < n) v |= (uint32_t)a[i + b] << (8 * b);
-    return v;
-  };
-  auto exponents = [&](const Where& w, const RowsOf& k, int ks) {
-    Exponents x{};
-    if constexpr (F8) {
-      const int64_t KB = (g.K + KS - 1) / KS;
-      const int p = w.p0 + wp * (BPo / C::WP);
-#pragma unroll
-      for (int j = 0; j < C::MQ; ++j) {
-        const int32_t r = GQ ? clip_token(k.r[j], (int32_t)(g.N - 1)) : k.r[j];
-        x.q[j] = four(g.q_exp, r * KB + ks, (GQ ? g.N : g.R) * KB);
-      }
-      if constexpr (LP == kInner) {
-        const int64_t PB = ((EPI == kSwiglu ? 2 : 1) * (int64_t)g.Pd + KS - 1) / KS;
-#pragma unroll
-        for (int i = 0; i < C::MP; ++i) {
-          const int64_t row = EPI == kSwiglu ? min(p + lrow, g.Pd - 1) + i * (int64_t)g.Pd : min(p + 32 * i + lrow, g.Pd - 1);
-          x.p[i] = four(g.p_exp, (w.e * PB + row / KS) * KB + ks, g.E * PB * KB);
-        }
-      } else {  // a wave's columns are in one block
-        const int64_t PB = (g.Pd + KS - 1) / KS;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          x.p[i] = g.p_exp[(w.e * KB + min((int64_t)ks + i, KB - 1)) * PB + min(p, g.Pd - 1) / KS];
-      }
-    }
-    return x;
-  };
-  // The values are there from here on (a loader's wait for them, later, would include its loads into LDS).
-  auto arrived = [](auto& v) {
-#pragma unroll
-    for (auto& u : v) asm volatile("" : "+v"(u));
   };
 
   using Frag = typename Mma<T>::Frag;
   struct Frags {
     Frag p[C::MP], q[C::MQ];
+    uint32_t ep[F8 ? C::MP : 1], eq[F8 ? C::MQ : 1];  // their exponents
   };
   // the operands of phase s of the stage in a buffer
   auto read = [&](Frags& f, int buf, int s) {
-    const char* sp = sm + buf * C::stage;
+    const char* sp = sm + buf * STAGE;
     const char* sq = sp + C::BP * kStageBytes;
 #pragma unroll
     for (int i = 0; i < C::MP; ++i) f.p[i] = rp.get(sp, i, s);
 #pragma unroll
     for (int j = 0; j < C::MQ; ++j) f.q[j] = rq.get(sq, j, s);
+    if constexpr (F8) {
+      const uint32_t* pe = reinterpret_cast<const uint32_t*>(sp + C::stage);
+#pragma unroll
+      for (int i = 0; i < C::MP; ++i) f.ep[i] = pe[wp * (C::BP / C::WP) + 32 * i + lrow];
+#pragma unroll
+      for (int j = 0; j < C::MQ; ++j) f.eq[j] = pe[C::BP + wq * (C::BQ / C::WQ) + 32 * j + lrow];
+    }
   };
 
   if constexpr (kLists<EPI, GP, GQ> > 0) {  // the first lists
@@ -1095,13 +1093,6 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
     __builtin_amdgcn_s_setprio(1);  // it begins to multiply later than the other wave of its SIMD
   }
   int buf = 0;
-  Exponents ex{}, ex_next{};
-  RowsOf rows_now{}, rows_next{};
-  if constexpr (F8) {
-    const Where w = locate(tile);
-    rows_now = rows_at(w);
-    ex_next = exponents(w, rows_now, 0);
-  }
   for (; tile < tile_end; tile += tile_step) {
     const Where w = locate(tile);
     if constexpr (EPI == kWeightGrad) {
@@ -1118,7 +1109,7 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
 #pragma unroll
         for (int i = 0; i < C::MP; ++i) {
           if constexpr (F8)
-            acc[i][j] = Mma<T>::mul(f.p[i], f.q[j], acc[i][j], ex.p[LP == kInner ? i : 0], ex.q[j]);
+            acc[i][j] = Mma<T>::mul(f.p[i], f.q[j], acc[i][j], f.ep[i], f.eq[j]);
           else
             acc[i][j] = Mma<T>::mul(f.p[i], f.q[j], acc[i][j]);
         }
@@ -1136,22 +1127,6 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
         clear(buf);
       }
       wave_barrier();
-      if constexpr (F8) {
-        if ((ks & 3) == 0) {
-          arrived(ex_next.p);
-          arrived(ex_next.q);
-          ex = ex_next;
-          if constexpr (LP == kOuter) ex.p[0] |= ex.p[1] << 8 | ex.p[2] << 16 | ex.p[3] << 24;
-          if (ks + 4 < w.nk) ex_next = exponents(w, rows_now, ks + 4);
-        }
-        if (tile + tile_step < tile_end) {  // the next tile's first ones, its tokens a stage or more ahead
-          if (ks == 0) rows_next = rows_at(locate(tile + tile_step));
-          if (ks == w.nk - 1) {
-            if constexpr (GQ) arrived(rows_next.r);
-            ex_next = exponents(locate(tile + tile_step), rows_next, 0);
-          }
-        }
-      }
       if (loader) load_stage();
 #pragma unroll
       for (int s = 0; s < kPhases<T>; ++s) {
@@ -1159,20 +1134,13 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
         read(f, buf, s);
         multiply(f);
       }
-      if constexpr (F8) {
-#pragma unroll
-        for (auto& v : ex.p) v >>= 8;
-#pragma unroll
-        for (auto& v : ex.q) v >>= 8;
-      }
       buf ^= 1;
     }
-    if constexpr (F8) rows_now = rows_next;
     if (kProbs<C, EPI> > 0 && prob_row >= 0 && prob_row < C::BQ) probs[prob_row] = prob;
     // The stage just used holds the waves' areas once every wave is done with it; it is loaded again
     // only after the next barrier.
     wave_barrier();
-    char* area = sm + (buf ^ 1) * C::stage + wave * (C::stage / C::waves);
+    char* area = sm + (buf ^ 1) * STAGE + wave * (C::stage / C::waves);
     const int qw = wq * (C::BQ / C::WQ), pw = wp * (C::BP / C::WP);
     if constexpr (EPI == kStore) {
       OT* y = static_cast<OT*>(g.out);
@@ -1208,7 +1176,7 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
       // through LDS.  Two lanes exchange halves, so that each stores 16 bytes.
       static_assert(C::MP == 2 && C::WP == 4, "a tile's activations are one block of a row");
       const int F = g.Pd, G = (F + kAct8Group - 1) / kAct8Group, GB = (F + kFp8Block - 1) / kFp8Block;
-      uint32_t* top = reinterpret_cast<uint32_t*>(sm + (buf ^ 1) * C::stage);  // [WP][BQ]
+      uint32_t* top = reinterpret_cast<uint32_t*>(sm + (buf ^ 1) * STAGE);  // [WP][BQ]
       const int h = lane >> 5, f0 = w.p0 + pw / 2, n = F - f0;
 #pragma unroll
       for (int j = 0; j < C::MQ; ++j) {
@@ -1403,7 +1371,7 @@ template <typename T, typename C, int LP, int LQ, int EPI, int LOAD, bool GP = f
 hipError_t launch_gemm(const ExpertGemm& g, hipStream_t s) {
   const void* kern = reinterpret_cast<const void*>(k_expert_gemm<T, C, LP, LQ, EPI, LOAD, GP, GQ>);
   auto lds_of = [](int E) {
-    return 2 * (size_t)C::stage + (kLists<EPI, GP, GQ> * kList + kProbs<C, EPI>) * 4 + (size_t)(E + 1) * 8;
+    return 2 * (size_t)kStage<T, C> + (kLists<EPI, GP, GQ> * kList + kProbs<C, EPI>) * 4 + (size_t)(E + 1) * 8;
   };
   // blocks per CU that the registers leave room for, and the kernel's LDS limit: set up once per device
   static std::atomic<int> by_registers[64];
