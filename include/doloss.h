@@ -542,7 +542,7 @@ do_status do_expert_swiglu_grad_fp8(const uint8_t* dy, const uint8_t* dy_exp, co
  * the products rounded to dtype; a token's sum is taken in an order that the
  * call's sizes and choices fix.
  */
-int64_t do_expert_layer_workspace(do_dtype dtype, int64_t N, int32_t E, int32_t k, int32_t F);
+int64_t do_expert_layer_workspace(do_dtype dtype, int64_t N, int32_t E, int32_t k, int32_t H, int32_t F);
 do_status do_expert_layer(const void* x, do_dtype dtype, const void* scores, do_dtype scores_dtype, const void* p,
                           do_dtype p_dtype, const void* w1, const uint8_t* w1_exp, const void* w2,
                           const uint8_t* w2_exp, int64_t N, int32_t E, int32_t k, int32_t H, int32_t F, void* y,

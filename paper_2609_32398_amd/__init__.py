@@ -104,7 +104,7 @@ def lib():
                                      st),
             "do_expert_swiglu_grad_fp8": ([vp, vp, vp, vp, vp, st, vp, vp, vp, vp, i64, i32, i32, i32, i32, vp, vp, vp,
                                            vp, vp, vp, i64, vp], st),
-            "do_expert_layer_workspace": ([st, i64, i32, i32, i32], i64),
+            "do_expert_layer_workspace": ([st, i64, i32, i32, i32, i32], i64),
             "do_expert_layer": ([vp, st, vp, st, vp, st, vp, vp, vp, vp, i64, i32, i32, i32, i32, vp, vp, i64, vp], st),
             "do_rem_allocate": ([vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp, vp], st),
             "do_rem_dispatch": ([vp, vp, i32, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp, vp], st),
@@ -979,7 +979,7 @@ def do_expert_layer(x: torch.Tensor, scores: torch.Tensor, k: int, w1, w2, p: to
         ptrs = (w1.data_ptr(), None, w2.data_ptr(), None)
     pp, pd = _probs_of(p, N, E)
     y = _out(out, "out", (N, H), x.dtype, x.device)
-    need = lib().do_expert_layer_workspace(_dtype_code(x), N, E, k, F)
+    need = lib().do_expert_layer_workspace(_dtype_code(x), N, E, k, H, F)
     ws = torch.empty(need, dtype=torch.uint8, device=x.device)
     _check(lib().do_expert_layer(x.data_ptr(), _dtype_code(x), scores.data_ptr(), _dtype_code(scores), pp, pd, *ptrs, N,
                                  E, k, H, F, y.data_ptr(), ws.data_ptr(), need, _stream()), "do_expert_layer")

@@ -517,11 +517,11 @@ DOLOSS_API do_status do_expert_swiglu_grad_fp8(const uint8_t* dy, const uint8_t*
 
 // ---- the layer of a few tokens --------------------------------------------------
 
-DOLOSS_API int64_t do_expert_layer_workspace(do_dtype dtype, int64_t N, int32_t E, int32_t k, int32_t F) {
+DOLOSS_API int64_t do_expert_layer_workspace(do_dtype dtype, int64_t N, int32_t E, int32_t k, int32_t H, int32_t F) {
   if ((dtype != DO_F32 && dtype != DO_BF16) || N < 1 || N > dol::kLayerTokens || E < 1 || E > dol::kMaxE || k < 1 ||
-      k > E || F < 1 || F > dol::kMaxWidth)
+      k > E || H < 1 || H > dol::kMaxWidth || F < 1 || F > dol::kMaxWidth)
     return 0;
-  return dol::expert_layer_bytes(dtype, N, E, k, F);
+  return dol::expert_layer_bytes(dtype, N, E, k, H, F);
 }
 
 DOLOSS_API do_status do_expert_layer(const void* x, do_dtype dtype, const void* scores, do_dtype scores_dtype,
@@ -547,8 +547,8 @@ DOLOSS_API do_status do_expert_layer(const void* x, do_dtype dtype, const void* 
     if (!aligned(p, size_of(p_dtype))) return set_error(DO_ERR_INVALID_ARG, "p is not aligned to its element size");
   }
   DO_TRY(check_ptr(workspace, 16, "workspace is NULL or not 16-byte aligned"));
-  if (workspace_bytes < do_expert_layer_workspace(dtype, N, E, k, F))
-    return set_error(DO_ERR_INVALID_ARG, "workspace is smaller than do_expert_layer_workspace(dtype, N, E, k, F)");
+  if (workspace_bytes < do_expert_layer_workspace(dtype, N, E, k, H, F))
+    return set_error(DO_ERR_INVALID_ARG, "workspace is smaller than do_expert_layer_workspace(dtype, N, E, k, H, F)");
   dol::LayerArgs a{};
   a.x = x;
   a.scores = scores;

@@ -21,13 +21,16 @@ namespace dol {
 namespace {
 
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+typedef uint32_t v2u __attribute__((ext_vector_type(2)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 
-constexpr int kUpWaves = 4, kDownWaves = 8;
+constexpr int kUpWaves = 4, kDownWaves = 4;
 constexpr int kTile = 16;     // rows and columns of a matrix instruction
 constexpr int kActs = 8;      // activations of a tile
-constexpr int kAhead = 4;     // steps whose loads are issued together
+constexpr int kMaxSplit = 16;       // blocks that share a column tile of the second kernel
+constexpr int kSplitBytes = 65536;  // of weights that such a block has at least
+constexpr int kManyTiles = 12;      // tiles a CU for which a wave takes a tile by itself
 
 __device__ __forceinline__ float sigmoid(float g) { return __builtin_amdgcn_rcpf(1.0f + __expf(-g)); }
 
@@ -36,8 +39,13 @@ template <typename T, bool W8>
 struct Form {
   static constexpr int W = W8 ? 16 : 16 / (int)sizeof(T);  // weights in a lane's 16 bytes
   static constexpr int X = W * (int)sizeof(T) / 16;        // 16-byte pieces of activations beside them
-  static constexpr int step = 4 * W;                       // k of a step
+  static constexpr int P = W8 ? 2 : 1;                     // pieces of weights in a step: 8 bits, a block's 128
+  static constexpr int piece = 4 * W;                      // k of four lanes' pieces
+  static constexpr int step = P * piece;
   using Element = std::conditional_t<W8, uint8_t, T>;
+  // steps that are on their way together, for NT tiles of activations: as many as leave four waves a SIMD
+  template <int NT>
+  static constexpr int ahead = std::max(2, std::min(8, 68 / (P * (4 + 4 * X * NT))));
 
   // acc[weight row 4 (lane / 16) + v][activation row lane % 16] += their products over the step's k
   static __device__ __forceinline__ v4f mul(v4u w, float s, const v4u* x, v4f acc) {
@@ -104,49 +112,91 @@ __device__ __forceinline__ v4u part(const E* p, int n) {
 }
 
 // A wave's products over steps [s0, s1) of a contraction of K: w is the lane's weight row, e its blocks' exponents, x
-// the lane's activation row of each of nt (NT at most) tiles.
+// the lane's activation row of each of NT tiles.
 template <typename T, bool W8, int NT>
-__device__ __forceinline__ void multiply(const typename Form<T, W8>::Element* w, const uint8_t* e, const T* const* x, int nt,
+__device__ __forceinline__ void multiply(const typename Form<T, W8>::Element* w, const uint8_t* e, const T* const* x,
                                          int K, int s0, int s1, int lane, v4f* acc) {
   using F = Form<T, W8>;
+  constexpr int D = F::template ahead<NT>;
   const int full = min(s1, K / F::step), mine = (lane >> 4) * F::W;
-  for (int s = s0; s < full; s += kAhead) {
-    v4u wv[kAhead], xv[kAhead][NT][F::X];
-    uint32_t ev[kAhead];
+  struct Step {
+    v4u w[F::P], x[F::P][NT][F::X];
+    uint32_t e;
+  };
+  // the lane's places in the step that is loaded next
+  const typename F::Element* wp = w + s0 * F::step + mine;
+  const uint8_t* ep = e + s0;
+  const T* xp[NT];
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      const int k = min(s + u, full - 1) * F::step + mine;
-      wv[u] = weights(w + k);
-      if constexpr (W8) ev[u] = e[k / kFp8Block];
+  for (int t = 0; t < NT; ++t) xp[t] = x[t] + s0 * F::step + mine;
+  auto load = [&](int u) {
+    Step n;
+#pragma unroll
+    for (int q = 0; q < F::P; ++q) {
+      const int k = u * F::step + q * F::piece;
+      n.w[q] = weights(wp + k);
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int i = 0; i < F::X; ++i) xv[u][t][i] = piece(x[t] + k + i * (F::W / F::X));
+        for (int i = 0; i < F::X; ++i) n.x[q][t][i] = piece(xp[t] + k + i * (F::W / F::X));
     }
+    n.e = W8 ? ep[u] : 0;
+    return n;
+  };
+  auto on = [&](int steps) {
+    wp += steps * F::step;
+    ep += W8 ? steps : 0;
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      if (s + u < full) {
-        const float sc = W8 ? fp8_scale(ev[u]) : 1.0f;
+    for (int t = 0; t < NT; ++t) xp[t] += steps * F::step;
+  };
+  auto use = [&](const Step& n) {
+    const float sc = W8 ? fp8_scale(n.e) : 1.0f;
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
-          if (t < nt) acc[t] = F::mul(wv[u], sc, xv[u][t], acc[t]);
+    for (int q = 0; q < F::P; ++q)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) acc[t] = F::mul(n.w[q], sc, n.x[q][t], acc[t]);
+  };
+  int left = full - s0;
+  if (left >= D) {  // D steps on their way at any time
+    Step ring[D];
+#pragma unroll
+    for (int u = 0; u < D; ++u) ring[u] = load(u);
+    on(D);
+    for (left -= D; left >= D; left -= D) {
+#pragma unroll
+      for (int u = 0; u < D; ++u) {
+        use(ring[u]);
+        ring[u] = load(u);
       }
+      on(D);
     }
+#pragma unroll
+    for (int u = 0; u < D; ++u) use(ring[u]);
+  }
+  if (left > 0) {  // fewer than D: as many again from the last one's place, which are not used
+    Step some[D - 1];
+#pragma unroll
+    for (int u = 0; u < D - 1; ++u) some[u] = load(min(u, left - 1));
+#pragma unroll
+    for (int u = 0; u < D - 1; ++u)
+      if (u < left) use(some[u]);
   }
   if (full < s1) {  // the last step, which ends inside
-    const int k = full * F::step + mine, n = K - k;
-    const v4u wv = n > 0 ? part(w + k, n) : v4u{0u, 0u, 0u, 0u};
-    const float sc = W8 && n > 0 ? fp8_scale(e[k / kFp8Block]) : 1.0f;
+    const float sc = W8 ? fp8_scale(e[full]) : 1.0f;
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      if (t >= nt) continue;
-      v4u xv[F::X];
+    for (int q = 0; q < F::P; ++q) {
+      const int k = full * F::step + q * F::piece + mine, n = K - k;
+      const v4u wv = n > 0 ? part(w + k, n) : v4u{0u, 0u, 0u, 0u};
 #pragma unroll
-      for (int i = 0; i < F::X; ++i) {
-        const int at = i * (F::W / F::X);
-        xv[i] = n > at ? part(x[t] + k + at, n - at) : v4u{0u, 0u, 0u, 0u};
+      for (int t = 0; t < NT; ++t) {
+        v4u xv[F::X];
+#pragma unroll
+        for (int i = 0; i < F::X; ++i) {
+          const int at = i * (F::W / F::X);
+          xv[i] = n > at ? part(x[t] + k + at, n - at) : v4u{0u, 0u, 0u, 0u};
+        }
+        acc[t] = F::mul(wv, sc, xv, acc[t]);
       }
-      acc[t] = F::mul(wv, sc, xv, acc[t]);
     }
   }
 }
@@ -209,15 +259,21 @@ __device__ __forceinline__ void list_tokens(u64 tokens, int lane, uint8_t* list)
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 }
 
-template <typename T, bool W8, int NT>
-__global__ __launch_bounds__(kUpWaves* kWave) void k_layer_up(const LayerArgs a) {
+// Waves a SIMD to leave registers for.
+template <int NT>
+constexpr int kOccupancy = NT == 1 ? 4 : 3;
+
+// NT: tiles of 16 tokens that share a pass over an expert's weights.  KW: waves that share a tile's contraction.
+template <typename T, bool W8, int NT, int KW>
+__global__ __launch_bounds__(kUpWaves* kWave, kOccupancy<NT>) void k_layer_up(const LayerArgs a) {
   using F = Form<T, W8>;
   constexpr int kThreads = kUpWaves * kWave;
-  __shared__ u64 tokens[kMaxE];
-  __shared__ Chosen chosen[kMaxE];
+  extern __shared__ __align__(16) char sm[];
+  Chosen* chosen = reinterpret_cast<Chosen*>(sm);           // [E]
+  u64* tokens = reinterpret_cast<u64*>(chosen + a.E);       // [E]
   __shared__ int32_t n_chosen;
   __shared__ uint8_t lists[kUpWaves][kWave];
-  __shared__ __align__(16) float red[2][kUpWaves][NT][kTile][kTile + 4];
+  __shared__ __align__(16) v4f red[2][KW][NT][kWave];  // KW > 1: the waves' sums, lane by lane
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   for (int e = tid; e < a.E; e += kThreads) tokens[e] = 0;
   __syncthreads();
@@ -249,21 +305,19 @@ __global__ __launch_bounds__(kUpWaves* kWave) void k_layer_up(const LayerArgs a)
   const int have = __builtin_amdgcn_readfirstlane(n_chosen);
   if (blockIdx.x == 0) {  // for the second kernel
     for (int i = tid; i < have; i += kThreads) a.chosen[i] = chosen[i];
+    for (int i = tid; i < (a.H + kTile - 1) / kTile; i += kThreads) a.arrived[i] = 0;
     if (tid == 0) *a.n_chosen = have;
   }
   const int C = (a.F + kActs - 1) / kActs, steps = (a.H + F::step - 1) / F::step;
-  const int s0 = wave * steps / kUpWaves, s1 = (wave + 1) * steps / kUpWaves;
+  const int part = wave % KW, s0 = part * steps / KW, s1 = (part + 1) * steps / KW;
   const int row = lane & 15;
+  constexpr int kAtOnce = kUpWaves / KW;  // tiles of a block
   int turn = 0;
-  for (int tile = blockIdx.x; tile < have * C; tile += gridDim.x, turn ^= 1) {
+  for (int tile = blockIdx.x * kAtOnce + wave / KW; tile < have * C; tile += gridDim.x * kAtOnce) {
     const Chosen ch = chosen[tile / C];
-    const int e = __builtin_amdgcn_readfirstlane(ch.e), n = __popcll(ch.tokens), f0 = tile % C * kActs;
+    const int e = __builtin_amdgcn_readfirstlane(ch.e), f0 = tile % C * kActs;
+    const int n = __builtin_amdgcn_readfirstlane(__popcll(ch.tokens));
     list_tokens(ch.tokens, lane, lists[wave]);
-    const int nt = (n + kTile - 1) / kTile;
-    const T* x[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-      x[t] = static_cast<const T*>(a.x) + (int64_t)lists[wave][min(t * kTile + row, n - 1)] * a.H;
     // 8 gate rows, then the 8 up rows beside them
     const int64_t wr = min(f0 + (row & 7), a.F - 1) + (row >> 3) * (int64_t)a.F;
     const auto* w = static_cast<const typename F::Element*>(a.w1) + ((int64_t)e * 2 * a.F + wr) * a.H;
@@ -272,61 +326,84 @@ __global__ __launch_bounds__(kUpWaves* kWave) void k_layer_up(const LayerArgs a)
       const int64_t PB = (2 * (int64_t)a.F + kFp8Block - 1) / kFp8Block, KB = (a.H + kFp8Block - 1) / kFp8Block;
       we = a.w1_exp + (e * PB + wr / kFp8Block) * KB;
     }
-    v4f acc[NT] = {};
-    multiply<T, W8, NT>(w, we, x, nt, a.H, s0, s1, lane, acc);
+    for (int r0 = 0; r0 < n; r0 += NT * kTile, turn ^= 1) {
+      const T* x[NT];
+      float p[NT];
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
-      if (t < nt) *reinterpret_cast<v4f*>(&red[turn][wave][t][row][(lane >> 4) * 4]) = acc[t];
-    __syncthreads();  // one a tile: the sums of the tile after next are written behind the next one
-    for (int i = tid; i < nt * kTile * kActs; i += kThreads) {
-      const int r = i / kActs, c = i % kActs;
-      if (r >= n || f0 + c >= a.F) continue;
-      float g = 0.0f, u = 0.0f;
-#pragma unroll
-      for (int v = 0; v < kUpWaves; ++v) {
-        g += red[turn][v][r / kTile][r % kTile][c];
-        u += red[turn][v][r / kTile][r % kTile][kActs + c];
+      for (int t = 0; t < NT; ++t) {
+        const int64_t token = lists[wave][min(r0 + t * kTile + row, n - 1)];
+        x[t] = static_cast<const T*>(a.x) + token * a.H;
+        p[t] = a.p == nullptr ? 1.0f
+               : a.p_bf16     ? bf16_float(static_cast<const uint16_t*>(a.p)[token * a.E + e])
+                              : static_cast<const float*>(a.p)[token * a.E + e];
       }
-      float p = 1.0f;
-      if (a.p != nullptr) {
-        const int64_t at = (int64_t)lists[wave][r] * a.E + e;
-        p = a.p_bf16 ? bf16_float(static_cast<const uint16_t*>(a.p)[at]) : static_cast<const float*>(a.p)[at];
-      }
-      const float h = p * (g * sigmoid(g)) * u;
-      T* d = static_cast<T*>(a.h) + (int64_t)(ch.first + r) * a.ldh + f0 + c;
-      // rounded to bf16 as an operand of the second product, as do_expert_swiglu does
-      if constexpr (sizeof(T) == 2)
-        *d = bf16_bits(h);
+      v4f acc[NT] = {};
+      if (NT == 1 || n - r0 <= kTile)
+        multiply<T, W8, 1>(w, we, x, a.H, s0, s1, lane, acc);
       else
-        *d = h;
+        multiply<T, W8, NT>(w, we, x, a.H, s0, s1, lane, acc);
+      if constexpr (KW > 1) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) red[turn][part][t][lane] = acc[t];
+        __syncthreads();  // one a turn: the sums of the turn after next are written behind the next one
+      }
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        if (KW > 1 && part != t) continue;  // one wave for each tile of tokens
+        v4f s = acc[t];
+        if constexpr (KW > 1) {
+          s = red[turn][0][t][lane];
+#pragma unroll
+          for (int v = 1; v < KW; ++v) s += red[turn][v][t][lane];
+        }
+        // lanes 0 to 31 hold four gates of a token each, the lanes 32 on their ups
+        const int r = r0 + t * kTile + row, c = f0 + (lane >> 4) * 4;
+        float h[4];
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          const float u = __shfl_xor(s[v], 32);
+          h[v] = p[t] * (s[v] * sigmoid(s[v])) * u;
+        }
+        if (lane < 32 && r < n) {
+          // rounded to bf16 as an operand of the second product, as do_expert_swiglu does; rows are whole pieces
+          T* d = static_cast<T*>(a.h) + (int64_t)(ch.first + r) * a.ldh + c;
+          if constexpr (sizeof(T) == 2) {
+            if (c < a.ldh) *reinterpret_cast<v2u*>(d) = v2u{bf16_pair(h[0], h[1]), bf16_pair(h[2], h[3])};
+          } else {
+            if (c < a.ldh) *reinterpret_cast<v4f*>(d) = v4f{h[0], h[1], h[2], h[3]};
+          }
+        }
+      }
     }
   }
 }
 
-template <typename T, bool W8, int NT>
-__global__ __launch_bounds__(kDownWaves* kWave) void k_layer_down(const LayerArgs a) {
+// TOK: tokens at most.  gridDim.y blocks share a column tile: each adds up its part of the experts, and the last one
+// to arrive adds the parts, in their order.
+template <typename T, bool W8, int NT, int TOK>
+__global__ __launch_bounds__(kDownWaves* kWave, kOccupancy<NT>) void k_layer_down(const LayerArgs a) {
   using F = Form<T, W8>;
   constexpr int kThreads = kDownWaves * kWave;
-  __shared__ Chosen chosen[kMaxE];
+  extern __shared__ __align__(16) char sm[];
+  Chosen* chosen = reinterpret_cast<Chosen*>(sm);
   __shared__ uint8_t lists[kDownWaves][kWave];
-  __shared__ __align__(16) float sums[kDownWaves][NT * kTile][kTile + 4];  // of a wave, by token and column
+  __shared__ __align__(16) float sums[kDownWaves][TOK][kTile + 4];  // of a wave, by token and column
+  __shared__ int32_t last;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, row = lane & 15;
-  const int have = *a.n_chosen;
-  for (int i = tid; i < have; i += kThreads) chosen[i] = a.chosen[i];
-  for (int i = lane; i < NT * kTile * (kTile + 4); i += kWave) (&sums[wave][0][0])[i] = 0.0f;
+  const int have = *a.n_chosen, S = gridDim.y;
+  // the list's end is not known yet: what lies behind it is loaded and not used
+  for (int i = tid; i < a.most; i += kThreads) chosen[i] = a.chosen[i];
+  for (int i = lane; i < TOK * (kTile + 4); i += kWave) (&sums[wave][0][0])[i] = 0.0f;
   __syncthreads();
   const int c0 = blockIdx.x * kTile;
-  const int steps = (a.F + F::step - 1) / F::step;
-  const int parts = max(1, kDownWaves / have);  // of an expert's contraction
-  for (int unit = wave; unit < have * parts; unit += kDownWaves) {
+  const int steps = (a.F + F::step - 1) / F::step, waves = S * kDownWaves;
+  const int parts = max(1, min(steps, waves / have));  // of an expert's contraction
+  for (int unit = blockIdx.y * kDownWaves + wave; unit < have * parts; unit += waves) {
     const Chosen ch = chosen[unit / parts];
-    const int e = __builtin_amdgcn_readfirstlane(ch.e), n = __popcll(ch.tokens), part = unit % parts;
+    const int e = __builtin_amdgcn_readfirstlane(ch.e), part = __builtin_amdgcn_readfirstlane(unit % parts);
+    const int n = __builtin_amdgcn_readfirstlane(__popcll(ch.tokens));
+    const int s0 = part * steps / parts, s1 = (part + 1) * steps / parts;
     list_tokens(ch.tokens, lane, lists[wave]);
-    const int nt = (n + kTile - 1) / kTile;
-    const T* x[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-      x[t] = static_cast<const T*>(a.h) + (int64_t)(ch.first + min(t * kTile + row, n - 1)) * a.ldh;
     const int64_t wr = min(c0 + row, a.H - 1);
     const auto* w = static_cast<const typename F::Element*>(a.w2) + ((int64_t)e * a.H + wr) * a.F;
     const uint8_t* we = nullptr;
@@ -334,75 +411,137 @@ __global__ __launch_bounds__(kDownWaves* kWave) void k_layer_down(const LayerArg
       const int64_t PB = (a.H + kFp8Block - 1) / kFp8Block, KB = (a.F + kFp8Block - 1) / kFp8Block;
       we = a.w2_exp + (e * PB + wr / kFp8Block) * KB;
     }
-    v4f acc[NT] = {};
-    multiply<T, W8, NT>(w, we, x, nt, a.F, part * steps / parts, (part + 1) * steps / parts, lane, acc);
+    for (int r0 = 0; r0 < n; r0 += NT * kTile) {
+      const T* x[NT];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      const int r = t * kTile + row;
-      if (r < n) {
-        v4f* s = reinterpret_cast<v4f*>(&sums[wave][lists[wave][r]][(lane >> 4) * 4]);
-        *s += acc[t];
+      for (int t = 0; t < NT; ++t)
+        x[t] = static_cast<const T*>(a.h) + (int64_t)(ch.first + min(r0 + t * kTile + row, n - 1)) * a.ldh;
+      v4f acc[NT] = {};
+      if (NT == 1 || n - r0 <= kTile)
+        multiply<T, W8, 1>(w, we, x, a.F, s0, s1, lane, acc);
+      else
+        multiply<T, W8, NT>(w, we, x, a.F, s0, s1, lane, acc);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const int r = r0 + t * kTile + row;
+        if (r < n) *reinterpret_cast<v4f*>(&sums[wave][lists[wave][r]][(lane >> 4) * 4]) += acc[t];
       }
     }
   }
   __syncthreads();
-  for (int i = tid; i < a.N * kTile; i += kThreads) {
-    const int t = i / kTile, c = i % kTile;
-    if (c0 + c >= a.H) continue;
-    float s = 0.0f;
-#pragma unroll
-    for (int v = 0; v < kDownWaves; ++v) s += sums[v][t][c];
-    T* d = static_cast<T*>(a.y) + (int64_t)t * a.H + c0 + c;
+  float* parted = a.parts + (int64_t)blockIdx.x * S * a.N * kTile;
+  const int all = a.N * kTile;
+  auto store = [&](int i, float s) {
+    const int t = i / kTile, c = c0 + i % kTile;
+    if (c >= a.H) return;
+    T* d = static_cast<T*>(a.y) + (int64_t)t * a.H + c;
     if constexpr (sizeof(T) == 2)
       *d = bf16_bits(s);
     else
       *d = s;
+  };
+  for (int i = tid; i < all; i += kThreads) {
+    float s = 0.0f;
+#pragma unroll
+    for (int v = 0; v < kDownWaves; ++v) s += sums[v][i / kTile][i % kTile];
+    if (S == 1)
+      store(i, s);
+    else
+      __hip_atomic_store(parted + blockIdx.y * all + i, s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  if (S == 1) return;
+  // The parts are stored and loaded past the L2 caches, which belong to an XCD each, so that they only have to be
+  // done before the count: a fence would write a whole cache back (60 us more).
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (tid == 0)
+    last = __hip_atomic_fetch_add(&a.arrived[blockIdx.x], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == S - 1;
+  __syncthreads();
+  if (!last) return;
+  for (int i = tid; i < all; i += kThreads) {
+    float s = 0.0f;
+    for (int v = 0; v < S; ++v) s += __hip_atomic_load(parted + v * all + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    store(i, s);
   }
 }
 
-template <typename T, bool W8, int NT>
-hipError_t launch(const LayerArgs& a, hipStream_t s) {
+template <typename T, bool W8, int NT, int KW>
+hipError_t launch_up(const LayerArgs& a, hipStream_t s) {
   static std::atomic<int> per_cu[64];
   const DevInfo di = device_info();
   if (di.device < 0 || di.device >= 64) return hipErrorInvalidDevice;
   int occ = per_cu[di.device].load(std::memory_order_acquire);
   if (occ == 0) {
     const hipError_t e =
-        hipOccupancyMaxActiveBlocksPerMultiprocessor(&occ, k_layer_up<T, W8, NT>, kUpWaves * kWave, 0);
+        hipOccupancyMaxActiveBlocksPerMultiprocessor(&occ, k_layer_up<T, W8, NT, KW>, kUpWaves * kWave, 0);
     if (e != hipSuccess) return e;
     if (occ < 1) return hipErrorLaunchOutOfResources;
     per_cu[di.device].store(occ, std::memory_order_release);
   }
   // at most this many tiles: how many experts are chosen is only known on the device
-  const int64_t tiles = std::min<int64_t>(a.E, (int64_t)a.N * a.k) * ((a.F + kActs - 1) / kActs);
-  const unsigned up = (unsigned)std::min<int64_t>(tiles, (int64_t)occ * di.cu_count);
-  hipLaunchKernelGGL((k_layer_up<T, W8, NT>), dim3(up), dim3(kUpWaves * kWave), 0, s, a);
-  const hipError_t e = hipGetLastError();
+  const int64_t tiles = (int64_t)a.most * ((a.F + kActs - 1) / kActs), blocks = (tiles * KW + kUpWaves - 1) / kUpWaves;
+  hipLaunchKernelGGL((k_layer_up<T, W8, NT, KW>), dim3((unsigned)std::min<int64_t>(blocks, (int64_t)occ * di.cu_count)),
+                     dim3(kUpWaves * kWave), (size_t)a.E * (sizeof(Chosen) + sizeof(u64)), s, a);
+  return hipGetLastError();
+}
+
+template <typename T, bool W8, int NT, int TOK>
+hipError_t launch(const LayerArgs& a, hipStream_t s) {
+  // one wave a tile where there are tiles for all waves of the GPU, else four
+  const int64_t tiles = (int64_t)a.most * ((a.F + kActs - 1) / kActs);
+  const bool many = tiles >= (int64_t)kManyTiles * device_info().cu_count;
+  const hipError_t e = many ? launch_up<T, W8, NT, 1>(a, s) : launch_up<T, W8, NT, kUpWaves>(a, s);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((k_layer_down<T, W8, NT>), dim3((unsigned)((a.H + kTile - 1) / kTile)), dim3(kDownWaves * kWave), 0,
-                     s, a);
+  hipLaunchKernelGGL((k_layer_down<T, W8, NT, TOK>), dim3((unsigned)((a.H + kTile - 1) / kTile), (unsigned)a.split),
+                     dim3(kDownWaves * kWave), (size_t)a.most * sizeof(Chosen), s, a);
   return hipGetLastError();
 }
 
 template <typename T, bool W8>
 hipError_t by_tokens(const LayerArgs& a, hipStream_t s) {
-  return a.N <= 16 ? launch<T, W8, 1>(a, s) : a.N <= 32 ? launch<T, W8, 2>(a, s) : launch<T, W8, 4>(a, s);
+  return a.N <= 16 ? launch<T, W8, 1, 16>(a, s) : launch<T, W8, 2, 64>(a, s);
 }
 
 }  // namespace
 
-// The workspace: how many experts are chosen, the list of them, the activations.
-int64_t expert_layer_bytes(do_dtype dt, int64_t N, int32_t E, int32_t k, int32_t F) {
-  const int64_t rows = N * k;
-  return 16 + std::min<int64_t>(E, rows) * (int64_t)sizeof(Chosen) + rows * layer_row(dt, F) * (dt == DO_F32 ? 4 : 2);
+// The workspace: how many experts are chosen, the list of them, how many blocks of a column tile have arrived, their
+// sums, the activations.
+namespace {
+struct LayerSpace {
+  int64_t chosen, arrived, parts, h, bytes;
+};
+LayerSpace layer_space(do_dtype dt, int64_t N, int32_t E, int32_t k, int32_t H, int32_t F) {
+  auto up = [](int64_t n) { return (n + 15) & ~int64_t(15); };
+  const int64_t rows = N * k, tiles = (H + kTile - 1) / kTile;
+  LayerSpace w;
+  w.chosen = 16;
+  w.arrived = w.chosen + std::min<int64_t>(E, rows) * (int64_t)sizeof(Chosen);
+  w.parts = w.arrived + up(tiles * 4);
+  w.h = w.parts + tiles * kMaxSplit * N * kTile * 4;
+  w.bytes = w.h + rows * layer_row(dt, F) * (dt == DO_F32 ? 4 : 2);
+  return w;
+}
+}  // namespace
+
+int64_t expert_layer_bytes(do_dtype dt, int64_t N, int32_t E, int32_t k, int32_t H, int32_t F) {
+  return layer_space(dt, N, E, k, H, F).bytes;
 }
 
 hipError_t launch_expert_layer(LayerArgs a, do_dtype dt, void* workspace, hipStream_t s) {
   char* ws = static_cast<char*>(workspace);
+  const LayerSpace w = layer_space(dt, a.N, a.E, a.k, a.H, a.F);
   a.n_chosen = reinterpret_cast<int32_t*>(ws);
-  a.chosen = reinterpret_cast<Chosen*>(ws + 16);
-  a.h = ws + 16 + std::min<int64_t>(a.E, (int64_t)a.N * a.k) * (int64_t)sizeof(Chosen);
+  a.chosen = reinterpret_cast<Chosen*>(ws + w.chosen);
+  a.arrived = reinterpret_cast<int32_t*>(ws + w.arrived);
+  a.parts = reinterpret_cast<float*>(ws + w.parts);
+  a.h = ws + w.h;
   a.ldh = layer_row(dt, a.F);
+  a.most = (int32_t)std::min<int64_t>(a.E, (int64_t)a.N * a.k);
+  // blocks that share a column tile of the second kernel: four a CU in all, each with 64 KiB of weights or more
+  const int64_t tiles = (a.H + kTile - 1) / kTile;
+  const int64_t bytes = (int64_t)a.most * kTile * a.F * (a.w1_exp != nullptr ? 1 : dt == DO_F32 ? 4 : 2);
+  a.split = (int32_t)std::max<int64_t>(
+      1, std::min({(int64_t)kMaxSplit, 4 * (int64_t)device_info().cu_count / tiles, bytes / kSplitBytes}));
   const bool w8 = a.w1_exp != nullptr;
   if (dt == DO_F32) return w8 ? by_tokens<float, true>(a, s) : by_tokens<float, false>(a, s);
   return w8 ? by_tokens<uint16_t, true>(a, s) : by_tokens<uint16_t, false>(a, s);

@@ -100,14 +100,18 @@ struct LayerArgs {
   void* y;                // [N][H]
   int32_t* n_chosen;      // workspace
   Chosen* chosen;
+  int32_t* arrived;       // [ceil(H / 16)]
+  float* parts;           // sums of the blocks that share a column tile
   void* h;                // activations, rows by expert
   int32_t N, E, k, H, F;
   int32_t ldh;            // elements of a row of h
+  int32_t most;           // experts that can be chosen
+  int32_t split;          // blocks that share a column tile of the second kernel
   int32_t scores_bf16, p_bf16;
 };
 // Rows of the activations are whole 16-byte pieces.
 inline int32_t layer_row(do_dtype dt, int32_t F) { return dt == DO_F32 ? (F + 3) & ~3 : (F + 7) & ~7; }
-int64_t expert_layer_bytes(do_dtype dt, int64_t N, int32_t E, int32_t k, int32_t F);
+int64_t expert_layer_bytes(do_dtype dt, int64_t N, int32_t E, int32_t k, int32_t H, int32_t F);
 hipError_t launch_expert_layer(LayerArgs a, do_dtype dt, void* workspace, hipStream_t s);
 
 // ---- bf16 and 8-bit conversions ---------------------------------------------

@@ -54,11 +54,13 @@ def test_products(dl):
 
 def test_layer(dl):
     L = dl.lib()
-    need = L.do_expert_layer_workspace(1, 10, 8, 2, 60)
-    assert need == 16 + 8 * 16 + 20 * 64 * 2
-    assert L.do_expert_layer_workspace(0, 1, 8, 2, 61) == 16 + 2 * 16 + 2 * 64 * 4
-    for bad in ((2, 10, 8, 2, 60), (1, 0, 8, 2, 60), (1, 65, 8, 2, 60), (1, 10, 0, 1, 60), (1, 10, 1025, 2, 60),
-                (1, 10, 8, 0, 60), (1, 10, 8, 9, 60), (1, 10, 8, 2, 0), (1, 10, 8, 2, 65537)):
+    need = L.do_expert_layer_workspace(1, 10, 8, 2, 64, 60)
+    assert need == 16 + 8 * 16 + 16 + 4 * 16 * 10 * 16 * 4 + 20 * 64 * 2
+    assert L.do_expert_layer_workspace(0, 1, 8, 2, 65, 61) == 16 + 2 * 16 + 32 + 5 * 16 * 16 * 4 + 2 * 64 * 4
+    good = (1, 10, 8, 2, 64, 60)
+    for i, v in ((0, 2), (1, 0), (1, 65), (2, 0), (2, 1025), (3, 0), (3, 9), (4, 0), (4, 65537), (5, 0), (5, 65537)):
+        bad = list(good)
+        bad[i] = v
         assert L.do_expert_layer_workspace(*bad) == 0
     _rejects(dl, "do_expert_layer",
              [FAKE, 1, FAKE, 0, FAKE, 0, FAKE, FAKE, FAKE, FAKE, 10, 8, 2, 64, 60, FAKE, FAKE, need, None], [
