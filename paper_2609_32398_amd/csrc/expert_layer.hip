@@ -209,43 +209,60 @@ __device__ __forceinline__ uint32_t rank_of(float v) {
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-template <int G>
-__device__ __forceinline__ u64 largest_of_group(u64 v) {
-#pragma unroll
-  for (int d = 1; d < G; d <<= 1) {
-    const u64 o = (u64)__shfl_xor((long long)v, d);
-    v = o > v ? o : v;
+// A value of another lane of the row of 16, or (scans) of the rows before; lanes without one get 0.
+template <int CTRL, int ROWS = 0xF>
+__device__ __forceinline__ uint32_t moved(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, false);
+}
+// op over the 16 lanes of a row, or all 64, in every lane.
+template <int G, typename F>
+__device__ __forceinline__ uint32_t over_group(uint32_t v, F&& op) {
+  v = op(v, moved<0x128>(v));  // rotations of the row by 8, 4, 2 and 1
+  v = op(v, moved<0x124>(v));
+  v = op(v, moved<0x122>(v));
+  v = op(v, moved<0x121>(v));
+  if constexpr (G == 64) {
+    auto of = [&](int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); };
+    v = op(op(of(0), of(16)), op(of(32), of(48)));
   }
+  return v;
+}
+// The sum of the lanes up to this one.
+__device__ __forceinline__ uint32_t running_sum(uint32_t v) {
+  v += moved<0x111>(v);  // shifts of the row by 1, 2, 4 and 8
+  v += moved<0x112>(v);
+  v += moved<0x114>(v);
+  v += moved<0x118>(v);
+  v += moved<0x142, 0xA>(v);  // the end of the row before to rows 1 and 3
+  v += moved<0x143, 0xC>(v);  // that of row 1 to rows 2 and 3
   return v;
 }
 
 // The tokens of each expert among every token's k best: larger scores first, equal ones by the lower expert.  G lanes
-// take a token, 16 experts a lane at most.
-template <int G, int THREADS>
+// take a token, P experts each.  A round finds the largest of what is left, and who has it.
+template <int G, int P, int THREADS>
 __device__ __forceinline__ void choose(const LayerArgs& a, u64* tokens) {
-  constexpr int P = 16;
   const int at = threadIdx.x % G;
   for (int t = threadIdx.x / G; t < a.N; t += THREADS / G) {
     uint32_t key[P];
     const int64_t row = (int64_t)t * a.E;
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-      key[i] = 0u;
       const int e = i * G + at;
-      if (i * G < a.E && e < a.E)
-        key[i] = rank_of(a.scores_bf16 ? bf16_float(static_cast<const uint16_t*>(a.scores)[row + e])
-                                       : static_cast<const float*>(a.scores)[row + e]);
+      const int64_t from = row + min(e, a.E - 1);
+      const float v = a.scores_bf16 ? bf16_float(static_cast<const uint16_t*>(a.scores)[from])
+                                    : static_cast<const float*>(a.scores)[from];
+      key[i] = e < a.E ? rank_of(v) : 0u;
     }
     for (int j = 0; j < a.k; ++j) {
-      uint32_t best = 0u, e = 0u;
+      uint32_t top = key[0];
 #pragma unroll
-      for (int i = 0; i < P; ++i) {
-        const bool more = key[i] > best;
-        best = more ? key[i] : best;
-        e = more ? (uint32_t)(i * G + at) : e;
-      }
-      const u64 top = largest_of_group<G>((u64)best << 32 | (0xFFFFFFFFu - e));
-      const uint32_t won = 0xFFFFFFFFu - (uint32_t)top;
+      for (int i = 1; i < P; ++i) top = max(top, key[i]);
+      top = over_group<G>(top, [](uint32_t x, uint32_t y) { return max(x, y); });
+      uint32_t won = ~0u;
+#pragma unroll
+      for (int i = P - 1; i >= 0; --i) won = key[i] == top ? (uint32_t)(i * G + at) : won;
+      won = over_group<G>(won, [](uint32_t x, uint32_t y) { return min(x, y); });
 #pragma unroll
       for (int i = 0; i < P; ++i) key[i] = won == (uint32_t)(i * G + at) ? 0u : key[i];
       if (at == 0) atomicOr(&tokens[won], (u64)1 << t);
@@ -277,23 +294,19 @@ __global__ __launch_bounds__(kUpWaves* kWave, kOccupancy<NT>) void k_layer_up(co
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   for (int e = tid; e < a.E; e += kThreads) tokens[e] = 0;
   __syncthreads();
-  if (a.E <= 256)
-    choose<16, kThreads>(a, tokens);
+  if (a.E <= 128)
+    choose<16, 8, kThreads>(a, tokens);
+  else if (a.E <= 256)
+    choose<16, 16, kThreads>(a, tokens);
   else
-    choose<64, kThreads>(a, tokens);
+    choose<64, 16, kThreads>(a, tokens);
   __syncthreads();
   if (wave == 0) {
     int rows = 0, have = 0;
     for (int e0 = 0; e0 < a.E; e0 += kWave) {
       const int e = e0 + lane;
       const u64 mine = e < a.E ? tokens[e] : 0;
-      int n = __popcll(mine);
-      const int own = n;
-#pragma unroll
-      for (int d = 1; d < kWave; d <<= 1) {
-        const int o = __shfl_up(n, d);
-        n += lane >= d ? o : 0;
-      }
+      const int own = __popcll(mine), n = (int)running_sum(own);
       const u64 some = __ballot(own > 0);
       if (own > 0) chosen[have + __popcll(some & (((u64)1 << lane) - 1))] = Chosen{e, rows + n - own, mine};
       rows += __builtin_amdgcn_readlane(n, 63);
@@ -459,8 +472,12 @@ __global__ __launch_bounds__(kDownWaves* kWave, kOccupancy<NT>) void k_layer_dow
   __syncthreads();
   if (!last) return;
   for (int i = tid; i < all; i += kThreads) {
-    float s = 0.0f;
-    for (int v = 0; v < S; ++v) s += __hip_atomic_load(parted + v * all + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    float v[kMaxSplit], s = 0.0f;  // all loaded before the first is used
+#pragma unroll
+    for (int u = 0; u < kMaxSplit; ++u)
+      v[u] = __hip_atomic_load(parted + min(u, S - 1) * all + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+    for (int u = 0; u < kMaxSplit; ++u) s += u < S ? v[u] : 0.0f;
     store(i, s);
   }
 }
@@ -537,11 +554,11 @@ hipError_t launch_expert_layer(LayerArgs a, do_dtype dt, void* workspace, hipStr
   a.h = ws + w.h;
   a.ldh = layer_row(dt, a.F);
   a.most = (int32_t)std::min<int64_t>(a.E, (int64_t)a.N * a.k);
-  // blocks that share a column tile of the second kernel: four a CU in all, each with 64 KiB of weights or more
+  // blocks that share a column tile of the second kernel: those that fit in all, each with 64 KiB of weights or more
   const int64_t tiles = (a.H + kTile - 1) / kTile;
   const int64_t bytes = (int64_t)a.most * kTile * a.F * (a.w1_exp != nullptr ? 1 : dt == DO_F32 ? 4 : 2);
   a.split = (int32_t)std::max<int64_t>(
-      1, std::min({(int64_t)kMaxSplit, 4 * (int64_t)device_info().cu_count / tiles, bytes / kSplitBytes}));
+      1, std::min({(int64_t)kMaxSplit, (a.N <= 16 ? 4 : 3) * (int64_t)device_info().cu_count / tiles, bytes / kSplitBytes}));
   const bool w8 = a.w1_exp != nullptr;
   if (dt == DO_F32) return w8 ? by_tokens<float, true>(a, s) : by_tokens<float, false>(a, s);
   return w8 ? by_tokens<uint16_t, true>(a, s) : by_tokens<uint16_t, false>(a, s);
