@@ -30,7 +30,6 @@ constexpr int kTile = 16;     // rows and columns of a matrix instruction
 constexpr int kActs = 8;      // activations of a tile
 constexpr int kMaxSplit = 16;       // blocks that share a column tile of the second kernel
 constexpr int kSplitBytes = 65536;  // of weights that such a block has at least
-constexpr int kManyTiles = 12;      // tiles a CU for which a wave takes a tile by itself
 
 __device__ __forceinline__ float sigmoid(float g) { return __builtin_amdgcn_rcpf(1.0f + __expf(-g)); }
 
@@ -243,17 +242,21 @@ __device__ __forceinline__ uint32_t running_sum(uint32_t v) {
 template <int G, int P, int THREADS>
 __device__ __forceinline__ void choose(const LayerArgs& a, u64* tokens) {
   const int at = threadIdx.x % G;
-  for (int t = threadIdx.x / G; t < a.N; t += THREADS / G) {
-    uint32_t key[P];
-    const int64_t row = (int64_t)t * a.E;
+  float next[P];  // the next token's scores
+  auto load = [&](int t) {
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-      const int e = i * G + at;
-      const int64_t from = row + min(e, a.E - 1);
-      const float v = a.scores_bf16 ? bf16_float(static_cast<const uint16_t*>(a.scores)[from])
-                                    : static_cast<const float*>(a.scores)[from];
-      key[i] = e < a.E ? rank_of(v) : 0u;
+      const int64_t from = (int64_t)min(t, a.N - 1) * a.E + min(i * G + at, a.E - 1);
+      next[i] = a.scores_bf16 ? bf16_float(static_cast<const uint16_t*>(a.scores)[from])
+                              : static_cast<const float*>(a.scores)[from];
     }
+  };
+  load(threadIdx.x / G);
+  for (int t = threadIdx.x / G; t < a.N; t += THREADS / G) {
+    uint32_t key[P];
+#pragma unroll
+    for (int i = 0; i < P; ++i) key[i] = i * G + at < a.E ? rank_of(next[i]) : 0u;
+    load(t + THREADS / G);
     for (int j = 0; j < a.k; ++j) {
       uint32_t top = key[0];
 #pragma unroll
@@ -280,8 +283,8 @@ __device__ __forceinline__ void list_tokens(u64 tokens, int lane, uint8_t* list)
 template <int NT>
 constexpr int kOccupancy = NT == 1 ? 4 : 3;
 
-// NT: tiles of 16 tokens that share a pass over an expert's weights.  KW: waves that share a tile's contraction.
-template <typename T, bool W8, int NT, int KW>
+// NT: tiles of 16 tokens that share a pass over an expert's weights.
+template <typename T, bool W8, int NT>
 __global__ __launch_bounds__(kUpWaves* kWave, kOccupancy<NT>) void k_layer_up(const LayerArgs a) {
   using F = Form<T, W8>;
   constexpr int kThreads = kUpWaves * kWave;
@@ -290,11 +293,13 @@ __global__ __launch_bounds__(kUpWaves* kWave, kOccupancy<NT>) void k_layer_up(co
   u64* tokens = reinterpret_cast<u64*>(chosen + a.E);       // [E]
   __shared__ int32_t n_chosen;
   __shared__ uint8_t lists[kUpWaves][kWave];
-  __shared__ __align__(16) v4f red[2][KW][NT][kWave];  // KW > 1: the waves' sums, lane by lane
+  __shared__ __align__(16) v4f red[2][kUpWaves][NT][kWave];  // the waves' sums, lane by lane
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   for (int e = tid; e < a.E; e += kThreads) tokens[e] = 0;
   __syncthreads();
-  if (a.E <= 128)
+  if (a.E <= 64)
+    choose<16, 4, kThreads>(a, tokens);
+  else if (a.E <= 128)
     choose<16, 8, kThreads>(a, tokens);
   else if (a.E <= 256)
     choose<16, 16, kThreads>(a, tokens);
@@ -322,11 +327,10 @@ __global__ __launch_bounds__(kUpWaves* kWave, kOccupancy<NT>) void k_layer_up(co
     if (tid == 0) *a.n_chosen = have;
   }
   const int C = (a.F + kActs - 1) / kActs, steps = (a.H + F::step - 1) / F::step;
-  const int part = wave % KW, s0 = part * steps / KW, s1 = (part + 1) * steps / KW;
+  const int s0 = wave * steps / kUpWaves, s1 = (wave + 1) * steps / kUpWaves;
   const int row = lane & 15;
-  constexpr int kAtOnce = kUpWaves / KW;  // tiles of a block
   int turn = 0;
-  for (int tile = blockIdx.x * kAtOnce + wave / KW; tile < have * C; tile += gridDim.x * kAtOnce) {
+  for (int tile = blockIdx.x; tile < have * C; tile += gridDim.x) {
     const Chosen ch = chosen[tile / C];
     const int e = __builtin_amdgcn_readfirstlane(ch.e), f0 = tile % C * kActs;
     const int n = __builtin_amdgcn_readfirstlane(__popcll(ch.tokens));
@@ -355,20 +359,15 @@ __global__ __launch_bounds__(kUpWaves* kWave, kOccupancy<NT>) void k_layer_up(co
         multiply<T, W8, 1>(w, we, x, a.H, s0, s1, lane, acc);
       else
         multiply<T, W8, NT>(w, we, x, a.H, s0, s1, lane, acc);
-      if constexpr (KW > 1) {
 #pragma unroll
-        for (int t = 0; t < NT; ++t) red[turn][part][t][lane] = acc[t];
-        __syncthreads();  // one a turn: the sums of the turn after next are written behind the next one
-      }
+      for (int t = 0; t < NT; ++t) red[turn][wave][t][lane] = acc[t];
+      __syncthreads();  // one a turn: the sums of the turn after next are written behind the next one
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        if (KW > 1 && part != t) continue;  // one wave for each tile of tokens
-        v4f s = acc[t];
-        if constexpr (KW > 1) {
-          s = red[turn][0][t][lane];
+        if (wave != t) continue;  // one wave for each tile of tokens
+        v4f s = red[turn][0][t][lane];
 #pragma unroll
-          for (int v = 1; v < KW; ++v) s += red[turn][v][t][lane];
-        }
+        for (int v = 1; v < kUpWaves; ++v) s += red[turn][v][t][lane];
         // lanes 0 to 31 hold four gates of a token each, the lanes 32 on their ups
         const int r = r0 + t * kTile + row, c = f0 + (lane >> 4) * 4;
         float h[4];
@@ -482,7 +481,7 @@ __global__ __launch_bounds__(kDownWaves* kWave, kOccupancy<NT>) void k_layer_dow
   }
 }
 
-template <typename T, bool W8, int NT, int KW>
+template <typename T, bool W8, int NT>
 hipError_t launch_up(const LayerArgs& a, hipStream_t s) {
   static std::atomic<int> per_cu[64];
   const DevInfo di = device_info();
@@ -490,24 +489,21 @@ hipError_t launch_up(const LayerArgs& a, hipStream_t s) {
   int occ = per_cu[di.device].load(std::memory_order_acquire);
   if (occ == 0) {
     const hipError_t e =
-        hipOccupancyMaxActiveBlocksPerMultiprocessor(&occ, k_layer_up<T, W8, NT, KW>, kUpWaves * kWave, 0);
+        hipOccupancyMaxActiveBlocksPerMultiprocessor(&occ, k_layer_up<T, W8, NT>, kUpWaves * kWave, 0);
     if (e != hipSuccess) return e;
     if (occ < 1) return hipErrorLaunchOutOfResources;
     per_cu[di.device].store(occ, std::memory_order_release);
   }
   // at most this many tiles: how many experts are chosen is only known on the device
-  const int64_t tiles = (int64_t)a.most * ((a.F + kActs - 1) / kActs), blocks = (tiles * KW + kUpWaves - 1) / kUpWaves;
-  hipLaunchKernelGGL((k_layer_up<T, W8, NT, KW>), dim3((unsigned)std::min<int64_t>(blocks, (int64_t)occ * di.cu_count)),
+  const int64_t tiles = (int64_t)a.most * ((a.F + kActs - 1) / kActs);
+  hipLaunchKernelGGL((k_layer_up<T, W8, NT>), dim3((unsigned)std::min<int64_t>(tiles, (int64_t)occ * di.cu_count)),
                      dim3(kUpWaves * kWave), (size_t)a.E * (sizeof(Chosen) + sizeof(u64)), s, a);
   return hipGetLastError();
 }
 
 template <typename T, bool W8, int NT, int TOK>
 hipError_t launch(const LayerArgs& a, hipStream_t s) {
-  // one wave a tile where there are tiles for all waves of the GPU, else four
-  const int64_t tiles = (int64_t)a.most * ((a.F + kActs - 1) / kActs);
-  const bool many = tiles >= (int64_t)kManyTiles * device_info().cu_count;
-  const hipError_t e = many ? launch_up<T, W8, NT, 1>(a, s) : launch_up<T, W8, NT, kUpWaves>(a, s);
+  const hipError_t e = launch_up<T, W8, NT>(a, s);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((k_layer_down<T, W8, NT, TOK>), dim3((unsigned)((a.H + kTile - 1) / kTile), (unsigned)a.split),
                      dim3(kDownWaves * kWave), (size_t)a.most * sizeof(Chosen), s, a);
