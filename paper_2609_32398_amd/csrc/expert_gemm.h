@@ -826,8 +826,10 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
   if (tile >= tile_end) return;
 
   constexpr bool VEC = LOAD != kElements, WIDE = LOAD == kWidePieces;
-  using LoaderP = std::conditional_t<VEC, PieceLoader<T, LP, C::BP, C::loaders, WIDE, GP>, ElementLoader<T, LP, C::BP, C::loaders>>;
-  using LoaderQ = std::conditional_t<VEC, PieceLoader<T, LQ, C::BQ, C::loaders, WIDE, GQ>, ElementLoader<T, LQ, C::BQ, C::loaders>>;
+  // all of them where rows of 8-bit elements go through registers
+  constexpr int LOADERS = F8 && !VEC ? C::threads : C::loaders;
+  using LoaderP = std::conditional_t<VEC, PieceLoader<T, LP, C::BP, LOADERS, WIDE, GP>, ElementLoader<T, LP, C::BP, LOADERS>>;
+  using LoaderQ = std::conditional_t<VEC, PieceLoader<T, LQ, C::BQ, LOADERS, WIDE, GQ>, ElementLoader<T, LQ, C::BQ, LOADERS>>;
   LoaderP lp;
   LoaderQ lq;
   Reader<T, LP, C::BP> rp;
@@ -876,10 +878,9 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
     }
   }
   // the tokens of a thread's rows of a tile, loaded ahead of start()
-  constexpr int NPE = F8 ? C::BP / C::loaders : 1, NQE = F8 ? (C::BQ + C::loaders - 1) / C::loaders : 1;
-  static_assert(!F8 || C::BP % C::loaders == 0);
+  constexpr int NE = F8 ? (C::BP + C::BQ + LOADERS - 1) / LOADERS : 1;  // exponents of a thread
   struct Tokens {
-    int32_t t[LoaderQ::N], of_exp[NQE];
+    int32_t t[LoaderQ::N], of_exp[NE];
   };
   auto tokens = [&](const Where& w) {
     Tokens k;
@@ -889,7 +890,8 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
         k.t[j] = g.q_token[w.r0 + min(LoaderQ::row(tid) + j * LoaderQ::RS, w.rows - 1)];
       if constexpr (F8) {
 #pragma unroll
-        for (int j = 0; j < NQE; ++j) k.of_exp[j] = g.q_token[w.r0 + min(tid + j * C::loaders, w.rows - 1)];
+        for (int j = 0; j < NE; ++j)
+          k.of_exp[j] = g.q_token[w.r0 + max(0, min(tid + j * LOADERS - C::BP, w.rows - 1))];
       }
     }
     return k;
@@ -901,27 +903,26 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
     return EPI == kSwiglu ? (i >> 6) * 32 + (i & 31) : i;
   };
   auto up_p = [](int j) { return EPI == kSwiglu ? (j * LoaderP::RS >> 5) & 1 : 0; };
-  // 8 bits: the exponents of operand rows tid, tid + loaders, .. of the tile, a byte for each stage
+  // 8 bits: the exponents of P's and then Q's rows of the tile, a byte of each for a stage; a wave's 64 are one operand's
   const int lrow = lane & 31;
-  const uint8_t *pexp[NPE], *qexp[NQE];
-  const int64_t KB = (g.K + KS - 1) / KS, pexp_step = LP == kInner ? 1 : (g.Pd + KS - 1) / KS;
+  const uint8_t* exps[NE];
+  const int64_t KB = (g.K + KS - 1) / KS, p_step = LP == kInner ? 1 : (g.Pd + KS - 1) / KS;
+  auto exps_of_p = [&](int j) { return tid - lane + j * LOADERS < C::BP; };
   auto start_exponents = [&](const Where& w, const Tokens& k) {
 #pragma unroll
-    for (int j = 0; j < NPE; ++j) {
-      const int i = tid + j * C::loaders;
-      if constexpr (LP == kInner) {
+    for (int j = 0; j < NE; ++j) {
+      const int i = tid + j * LOADERS;
+      if (!exps_of_p(j)) {
+        const int r = min(i - C::BP, w.rows - 1);
+        exps[j] = g.q_exp + (GQ ? clip_token(k.of_exp[j], (int32_t)(g.N - 1)) : w.r0 + r) * KB;
+      } else if constexpr (LP == kInner) {
         const int64_t PB = ((EPI == kSwiglu ? 2 : 1) * (int64_t)g.Pd + KS - 1) / KS;
         const int64_t row = EPI == kSwiglu ? min(w.p0 + (i >> 6) * 32 + (i & 31), g.Pd - 1) + (i >> 5 & 1) * (int64_t)g.Pd
                                            : min(w.p0 + i, g.Pd - 1);
-        pexp[j] = g.p_exp + (w.e * PB + row / KS) * KB;
+        exps[j] = g.p_exp + (w.e * PB + row / KS) * KB;
       } else {
-        pexp[j] = g.p_exp + w.e * KB * pexp_step + min(w.p0 + i, g.Pd - 1) / KS;
+        exps[j] = g.p_exp + w.e * KB * p_step + min(w.p0 + i, g.Pd - 1) / KS;
       }
-    }
-#pragma unroll
-    for (int j = 0; j < NQE; ++j) {
-      const int i = min(tid + j * C::loaders, w.rows - 1);
-      qexp[j] = g.q_exp + (GQ ? clip_token(k.of_exp[j], (int32_t)(g.N - 1)) : w.r0 + i) * KB;
     }
   };
   auto start = [&](const Where& w, const Tokens& k) {
@@ -940,7 +941,9 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
           lp.start_inner(tid, g.K, we, g.ldp, w.p0, g.Pd - 1);
         else
           lp.start_rows(tid, g.K, we, g.ldp, [&](int j) {
-            return min(w.p0 + LoaderP::row(tid) + far_p(j), g.Pd - 1) + up_p(j) * g.Pd;
+            const int i = LoaderP::row(tid) + j * LoaderP::RS;
+            return EPI == kSwiglu ? min(w.p0 + (i >> 6) * 32 + (i & 31), g.Pd - 1) + (i >> 5 & 1) * g.Pd
+                                  : min(w.p0 + i, g.Pd - 1);
           });
       } else {
         lp.start_outer(tid, g.K, P + (int64_t)w.e * g.K * g.ldp, g.ldp, w.p0, g.Pd, nullptr, 0, nullptr);
@@ -960,7 +963,7 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
   const uint32_t wave_lds = lds_base + (uint32_t)(tid & ~63) * 16;
 
   // The loaders run a stage ahead of the products, through the tiles in the same order.
-  const bool loader = tid < C::loaders;
+  const bool loader = tid < LOADERS;
   int load_tile = tile;  // the first one to load
   Where wl;
   Tokens kn;
@@ -1012,35 +1015,22 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
   auto load_exponents = [&] {
     const uint32_t dst = lds_base + load_slot * STAGE + C::stage + (tid & ~63) * 4;
 #pragma unroll
-    for (int j = 0; j < NPE; ++j) {
-      byte_to_lds(pexp[j], __builtin_amdgcn_readfirstlane(dst + j * C::loaders * 4));
-      pexp[j] += pexp_step;
-    }
-#pragma unroll
-    for (int j = 0; j < NQE; ++j) {
-      if (tid - lane + j * C::loaders < C::BQ)
-        byte_to_lds(qexp[j], __builtin_amdgcn_readfirstlane(dst + (C::BP + j * C::loaders) * 4));
-      ++qexp[j];
+    for (int j = 0; j < NE; ++j) {
+      if (tid - lane + j * LOADERS < C::BP + C::BQ)
+        byte_to_lds(exps[j], __builtin_amdgcn_readfirstlane(dst + j * LOADERS * 4));
     }
   };
-  auto load_stage = [&] {
-    if (!loading) return;
-    if constexpr (F8) load_exponents();
-    if constexpr (!VEC && kLoads <= 12) {
-      v4u vp[LoaderP::N], vq[LoaderQ::N];
-      char* st = sm + load_slot * STAGE;
-      lp.template fetch<0, LoaderP::N>(vp);
-      lq.template fetch<0, LoaderQ::N>(vq);
-      lp.template put<0, LoaderP::N>(tid, st, vp);
-      lq.template put<0, LoaderQ::N>(tid, st + C::BP * kStageBytes, vq);
-    } else {
-      each<kLoads>([&](auto i) { load(i); });
-    }
+  // The loaders go on to the stage after the one that has been loaded.
+  auto next_stage = [&] {
     load_slot ^= 1;
     have = load_have;
     if (--load_left > 0) {
       lp.next(tid);
       lq.next(tid);
+      if constexpr (F8) {
+#pragma unroll
+        for (int j = 0; j < NE; ++j) exps[j] += exps_of_p(j) ? p_step : 1;
+      }
       load_have -= KS;
     } else {
       loading = next_tile < tile_end;
@@ -1051,6 +1041,36 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
         next_tile = look(next_tile + tile_step);
       }
     }
+  };
+  // Elements: a stage's pieces, on their way to registers, and then to LDS.
+  constexpr bool ATONCE = !VEC && kLoads <= 12;
+  struct Pieces {
+    v4u p[ATONCE ? LoaderP::N : 1], q[ATONCE ? LoaderQ::N : 1];
+  };
+  auto fetch = [&](Pieces& v) {
+    if constexpr (ATONCE) {
+      lp.template fetch<0, LoaderP::N>(v.p);
+      lq.template fetch<0, LoaderQ::N>(v.q);
+    }
+  };
+  auto put = [&](Pieces& v) {
+    if constexpr (ATONCE) {
+      char* st = sm + load_slot * STAGE;
+      lp.template put<0, LoaderP::N>(tid, st, v.p);
+      lq.template put<0, LoaderQ::N>(tid, st + C::BP * kStageBytes, v.q);
+    }
+  };
+  auto load_stage = [&] {
+    if (!loading) return;
+    if constexpr (F8) load_exponents();
+    if constexpr (ATONCE) {
+      Pieces v;
+      fetch(v);
+      put(v);
+    } else {
+      each<kLoads>([&](auto i) { load(i); });
+    }
+    next_stage();
   };
   // Once the loads of the stage in a buffer have arrived: zeros past the end of a short one.
   auto clear = [&](int b) {
@@ -1090,7 +1110,7 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
   }
   if (loader) {
     load_stage();
-    __builtin_amdgcn_s_setprio(1);  // it begins to multiply later than the other wave of its SIMD
+    if constexpr (!F8 || VEC) __builtin_amdgcn_s_setprio(1);  // it begins to multiply later than the other wave of its SIMD
   }
   int buf = 0;
   for (; tile < tile_end; tile += tile_step) {
@@ -1103,22 +1123,34 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
     for (int i = 0; i < C::MP; ++i)
 #pragma unroll
       for (int j = 0; j < C::MQ; ++j) acc[i][j] = v16f{};
-    auto multiply = [&](const Frags& f) {
+    // the products of column tile j of the phase's operands
+    auto multiply = [&](const Frags& f, int j) {
 #pragma unroll
-      for (int j = 0; j < C::MQ; ++j)
-#pragma unroll
-        for (int i = 0; i < C::MP; ++i) {
-          if constexpr (F8)
-            acc[i][j] = Mma<T>::mul(f.p[i], f.q[j], acc[i][j], f.ep[i], f.eq[j]);
-          else
-            acc[i][j] = Mma<T>::mul(f.p[i], f.q[j], acc[i][j]);
+      for (int i = 0; i < C::MP; ++i) {
+        v16f& a = acc[i][j];
+        if constexpr (F8) {
+          a = Mma<T>::mul(f.p[i], f.q[j], a, f.ep[i], f.eq[j]);
+          // here, and not behind a branch to come with all operands held until then
+          if constexpr (!VEC) asm volatile("" : "+v"(a));
+        } else {
+          a = Mma<T>::mul(f.p[i], f.q[j], a);
         }
+      }
+    };
+    auto products = [&] {
+#pragma unroll
+      for (int s = 0; s < kPhases<T>; ++s) {
+        Frags f;
+        read(f, buf, s);
+#pragma unroll
+        for (int j = 0; j < C::MQ; ++j) multiply(f, j);
+      }
     };
     // A tile's row probabilities: loaded now, by waves that load nothing else where there are some (a wait
     // for them would include all loads before), used after the last stage.
     float prob = 0.0f;
-    const int prob_row = tid - (C::threads - C::loaders);
-    static_assert(kProbs<C, EPI> <= C::loaders);
+    const int prob_row = tid - (C::threads - LOADERS);
+    static_assert(kProbs<C, EPI> <= LOADERS);
     if (kProbs<C, EPI> > 0 && prob_row >= 0 && prob_row < w.rows && prob_row < C::BQ)
       prob = row_prob(g, w.r0 + prob_row, w.e);
     for (int ks = 0; ks < w.nk; ++ks) {
@@ -1127,12 +1159,22 @@ __global__ __launch_bounds__(C::threads, C::occ) void k_expert_gemm(const Expert
         clear(buf);
       }
       wave_barrier();
-      if (loader) load_stage();
-#pragma unroll
-      for (int s = 0; s < kPhases<T>; ++s) {
-        Frags f;
-        read(f, buf, s);
-        multiply(f);
+      if constexpr (!F8 || VEC) {
+        if (loader) load_stage();
+        products();
+      } else {  // the next stage on its way to registers meanwhile
+        // waited for before loads are under way, which a wait would include
+        if (kProbs<C, EPI> > 0 && ks == 1) asm volatile("" : "+v"(prob));
+        Pieces v;
+        if (loading) {
+          load_exponents();
+          fetch(v);
+        }
+        products();
+        if (loading) {
+          put(v);
+          next_stage();
+        }
       }
       buf ^= 1;
     }
