@@ -137,9 +137,9 @@ def _check(status: int, where: str):
         raise DoLossError(status, where, lib().do_last_error().decode())
 
 
-def _stream() -> ctypes.c_void_p:
-    # the handle alone: 0.4 us, where a torch.cuda.Stream around it takes 3
-    return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
+def _stream() -> int:
+    # the handle alone: 0.2 us, where a torch.cuda.Stream around it takes 3
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def _dtype_code(t: torch.Tensor) -> int:
@@ -154,6 +154,10 @@ def _want(t: torch.Tensor, name: str, shape=None, dtypes=None, numel=None):
     """Checks a tensor argument before its pointer reaches the library: shape
     (or element count), dtype and contiguity first, then that it lives on the
     current GPU.  Every failure raises ValueError before any launch."""
+    # what is right passes in one expression: 0.4 us, where the checks one by one take 0.8
+    if (isinstance(t, torch.Tensor) and (shape is None or t.shape == shape) and (dtypes is None or t.dtype in dtypes)
+            and numel is None and t.is_contiguous() and t.is_cuda and t.get_device() == torch._C._cuda_getDevice()):
+        return
     if not isinstance(t, torch.Tensor):
         raise ValueError(f"{name} must be a torch.Tensor")
     if shape is not None and tuple(t.shape) != tuple(shape):
@@ -821,12 +825,13 @@ def _want_fp8(a: Fp8, name: str, shape, weights: bool):
     _want(a.e, f"{name}.e", shape=(*lead, _blocks(shape[-1])), dtypes=_U8)
 
 
-def _fp8_weights(w: Fp8, name: str, E: int | None):
+def _fp8_weights(w: Fp8, name: str, E: int):
     """(O, I) of the weights [E, O, I] of an Fp8, after checking them."""
-    if not isinstance(w, Fp8) or not isinstance(w.q, torch.Tensor) or w.q.dim() != 3 or E not in (None, w.q.shape[0]):
-        raise ValueError(f"{name} must be an Fp8 of shape [{'E' if E is None else E}, O, I] (do_fp8_pack with weights=True)")
-    _want_fp8(w, name, tuple(w.q.shape), True)
-    return w.q.shape[1], w.q.shape[2]
+    if not isinstance(w, Fp8) or not isinstance(w.q, torch.Tensor) or w.q.dim() != 3 or w.q.shape[0] != E:
+        raise ValueError(f"{name} must be an Fp8 of shape [{E}, O, I] (do_fp8_pack with weights=True)")
+    shape = w.q.shape
+    _want_fp8(w, name, shape, True)
+    return shape[1], shape[2]
 
 
 def do_fp8_pack(x: torch.Tensor, weights: bool = False) -> Fp8:
