@@ -156,7 +156,7 @@ def _want(t: torch.Tensor, name: str, shape=None, dtypes=None, numel=None):
     current GPU.  Every failure raises ValueError before any launch."""
     # what is right passes in one expression: 0.4 us, where the checks one by one take 0.8
     if (isinstance(t, torch.Tensor) and (shape is None or t.shape == shape) and (dtypes is None or t.dtype in dtypes)
-            and numel is None and t.is_contiguous() and t.is_cuda and t.get_device() == torch._C._cuda_getDevice()):
+            and numel is None and t.is_cuda and t.is_contiguous() and t.get_device() == torch._C._cuda_getDevice()):
         return
     if not isinstance(t, torch.Tensor):
         raise ValueError(f"{name} must be a torch.Tensor")
@@ -171,6 +171,18 @@ def _want(t: torch.Tensor, name: str, shape=None, dtypes=None, numel=None):
     why = _device_problem(t)
     if why:
         raise ValueError(f"{name} {why}")
+
+
+def _held(*tensors: torch.Tensor) -> bool:
+    """Whether the library can take these as they lie, on the current GPU."""
+    for t in tensors:
+        if not (t.is_cuda and t.is_contiguous()):
+            return False
+    device = torch._C._cuda_getDevice()
+    for t in tensors:
+        if t.get_device() != device:
+            return False
+    return True
 
 
 def _device_problem(t: torch.Tensor) -> str | None:
@@ -609,6 +621,14 @@ def _row_sizes(rows: ExpertRows):
     if not isinstance(rows, ExpertRows):
         raise ValueError("rows must be an ExpertRows (do_expert_rows)")
     offsets, row_token, token_row, token_expert = rows
+    # right ones in one expression, as in _want
+    if (isinstance(token_row, torch.Tensor) and isinstance(offsets, torch.Tensor) and isinstance(row_token, torch.Tensor)
+            and isinstance(token_expert, torch.Tensor) and token_row.dim() == 2 and offsets.dim() == 1):
+        N, k = shape = token_row.shape
+        if (row_token.shape == (N * k,) and token_expert.shape == shape
+                and offsets.dtype == row_token.dtype == token_row.dtype == token_expert.dtype == torch.int32
+                and _held(offsets, row_token, token_row, token_expert)):
+            return N, offsets.shape[0] - 1, k, N * k
     _want(token_row, "rows.token_row", dtypes=_I32)
     if not isinstance(offsets, torch.Tensor) or token_row.dim() != 2 or offsets.dim() != 1:
         raise ValueError("rows.token_row must have shape [N, k] and rows.offsets shape [E + 1]")
@@ -820,9 +840,14 @@ def _want_fp8(a: Fp8, name: str, shape, weights: bool):
     """Checks an Fp8 operand whose values have `shape`."""
     if not isinstance(a, Fp8):
         raise ValueError(f"{name} must be an Fp8 (do_fp8_pack)")
-    _want(a.q, f"{name}.q", shape=shape, dtypes=_F8)
+    q, e = a
     lead = (*shape[:-2], _blocks(shape[-2])) if weights else shape[:-1]
-    _want(a.e, f"{name}.e", shape=(*lead, _blocks(shape[-1])), dtypes=_U8)
+    of_e = (*lead, _blocks(shape[-1]))
+    if (isinstance(q, torch.Tensor) and isinstance(e, torch.Tensor) and q.shape == shape and e.shape == of_e
+            and q.dtype == torch.float8_e4m3fn and e.dtype == torch.uint8 and _held(q, e)):
+        return
+    _want(q, f"{name}.q", shape=shape, dtypes=_F8)
+    _want(e, f"{name}.e", shape=of_e, dtypes=_U8)
 
 
 def _fp8_weights(w: Fp8, name: str, E: int):
@@ -841,14 +866,14 @@ def do_fp8_pack(x: torch.Tensor, weights: bool = False) -> Fp8:
         raise ValueError(f"x must be a tensor of shape {'[..., O, I]' if weights else '[..., W]'} with at least one element")
     _want(x, "x", dtypes=_SCORE_DTYPES)
     W = x.shape[-1]
-    q = torch.empty(x.shape, dtype=torch.float8_e4m3fn, device=x.device)
+    q = torch.empty_like(x, dtype=torch.float8_e4m3fn)
     if weights:
         O = x.shape[-2]
-        a = Fp8(q, torch.empty((*x.shape[:-2], _blocks(O), _blocks(W)), dtype=torch.uint8, device=x.device))
+        a = Fp8(q, x.new_empty((*x.shape[:-2], _blocks(O), _blocks(W)), dtype=torch.uint8))
         _check(lib().do_fp8_pack_weights(x.data_ptr(), _dtype_code(x), x.numel() // (O * W), O, W, q.data_ptr(),
                                          a.e.data_ptr(), _stream()), "do_fp8_pack_weights")
     else:
-        a = Fp8(q, torch.empty((*x.shape[:-1], _blocks(W)), dtype=torch.uint8, device=x.device))
+        a = Fp8(q, x.new_empty((*x.shape[:-1], _blocks(W)), dtype=torch.uint8))
         _check(lib().do_fp8_pack(x.data_ptr(), _dtype_code(x), x.numel() // W, W, q.data_ptr(), a.e.data_ptr(),
                                  _stream()), "do_fp8_pack")
     return a
@@ -864,7 +889,7 @@ def do_fp8_unpack(a: Fp8, dtype: torch.dtype, out: torch.Tensor | None = None) -
     # one row is a block of weights as well: both forms have the same exponents
     weights = len(shape) > 1 and isinstance(a.e, torch.Tensor) and a.e.shape[-2:-1] != shape[-2:-1]
     _want_fp8(a, "a", shape, weights)
-    x = _out(out, "out", shape, dtype, a.q.device)
+    x = torch.empty_like(a.q, dtype=dtype) if out is None else _out(out, "out", shape, dtype, a.q.device)
     W = shape[-1]
     if weights:
         O = shape[-2]
@@ -892,7 +917,8 @@ def do_expert_matmul_fp8(x: Fp8, w: Fp8, rows: ExpertRows | None, gather: bool =
         N, E, k, R = _row_sizes(rows)
         O, I = _fp8_weights(w, "w", E)
     _want_fp8(x, "x", (N if gather else R, O if transposed else I), False)
-    y = _out(out, "out", (R, I if transposed else O), torch.bfloat16, w.q.device)
+    of_y = (R, I if transposed else O)
+    y = w.q.new_empty(of_y, dtype=torch.bfloat16) if out is None else _out(out, "out", of_y, torch.bfloat16, w.q.device)
     _check(lib().do_expert_matmul_fp8(x.q.data_ptr(), x.e.data_ptr(), w.q.data_ptr(), w.e.data_ptr(),
                                       rows.offsets.data_ptr() if rows is not None else None,
                                       rows.row_token.data_ptr() if gather else None, N, R, E, O, I, int(transposed),
@@ -909,13 +935,11 @@ def do_expert_swiglu_fp8(x: Fp8, w1: Fp8, rows: ExpertRows, p: torch.Tensor | No
     F = F2 // 2
     _want_fp8(x, "x", (N, H), False)
     pp, pd = _probs_of(p, N, E)
-    dev = w1.q.device
-    h = Fp8(torch.empty((R, F), dtype=torch.float8_e4m3fn, device=dev),
-            torch.empty((R, _blocks(F)), dtype=torch.uint8, device=dev))
+    new = w1.q.new_empty
+    h = Fp8(new((R, F)), new((R, _blocks(F)), dtype=torch.uint8))
     kept = None
     if checkpoint:
-        kept = Act8(torch.empty((R, 2, F), dtype=torch.int8, device=dev),
-                    torch.empty((R, 2, -(-F // ACT8_GROUP)), dtype=torch.uint8, device=dev))
+        kept = Act8(new((R, 2, F), dtype=torch.int8), new((R, 2, -(-F // ACT8_GROUP)), dtype=torch.uint8))
     _check(lib().do_expert_swiglu_fp8(x.q.data_ptr(), x.e.data_ptr(), w1.q.data_ptr(), w1.e.data_ptr(), pp, pd,
                                       rows.offsets.data_ptr(), rows.row_token.data_ptr(), N, R, E, H, F,
                                       h.q.data_ptr(), h.e.data_ptr(), kept.q.data_ptr() if kept else None,
@@ -930,15 +954,14 @@ def do_expert_swiglu_grad_fp8(dy: Fp8, w2: Fp8, rows: ExpertRows, checkpoint: Ac
     _want_fp8(dy, "dy", (N, H), False)
     _want_checkpoint(checkpoint, R, F)
     pp, pd = _probs_of(p, N, E)
-    dev = w2.q.device
-    da = torch.empty((R, 2 * F), dtype=torch.bfloat16, device=dev)
-    h = torch.empty((R, F), dtype=torch.bfloat16, device=dev)
+    new = w2.q.new_empty
+    da, h = new((R, 2 * F), dtype=torch.bfloat16), new((R, F), dtype=torch.bfloat16)
     dp = ws = None
     need = 0
     if p is not None:
-        dp = torch.empty((N, E), dtype=p.dtype, device=dev)
+        dp = torch.empty_like(p)
         need = lib().do_expert_swiglu_grad_workspace(R, F)
-        ws = torch.empty(need, dtype=torch.uint8, device=dev)
+        ws = new(need, dtype=torch.uint8)
     _check(lib().do_expert_swiglu_grad_fp8(dy.q.data_ptr(), dy.e.data_ptr(), w2.q.data_ptr(), w2.e.data_ptr(), pp, pd,
                                            rows.offsets.data_ptr(), rows.row_token.data_ptr(),
                                            rows.token_row.data_ptr(), rows.token_expert.data_ptr(), N, E, k, H, F,
@@ -983,9 +1006,9 @@ def do_expert_layer(x: torch.Tensor, scores: torch.Tensor, k: int, w1, w2, p: to
         _operand(w2, "w2", (E, H, F), x)
         ptrs = (w1.data_ptr(), None, w2.data_ptr(), None)
     pp, pd = _probs_of(p, N, E)
-    y = _out(out, "out", (N, H), x.dtype, x.device)
+    y = torch.empty_like(x) if out is None else _out(out, "out", (N, H), x.dtype, x.device)
     need = lib().do_expert_layer_workspace(_dtype_code(x), N, E, k, H, F)
-    ws = torch.empty(need, dtype=torch.uint8, device=x.device)
+    ws = x.new_empty(need, dtype=torch.uint8)
     _check(lib().do_expert_layer(x.data_ptr(), _dtype_code(x), scores.data_ptr(), _dtype_code(scores), pp, pd, *ptrs, N,
                                  E, k, H, F, y.data_ptr(), ws.data_ptr(), need, _stream()), "do_expert_layer")
     return y
