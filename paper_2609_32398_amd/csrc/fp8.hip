@@ -154,11 +154,12 @@ __device__ __forceinline__ void fp8_values4(uint32_t q, float s, float* v) {
   v[3] = hi[1] * s;
 }
 
-// Back: 16 elements a thread.  OB: 128 rows share an exponent (weights; 0: each row has its own).
+// Back: a thread writes 16 bytes, so that a wave's stores are one run (with 16 elements a thread, in two stores, 65,536 x
+// 2,048 bf16 took 98 us).  OB: 128 rows share an exponent (weights; 0: each row has its own).
 template <typename T, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void k_fp8_unpack(const uint8_t* q, const uint8_t* e, int64_t pieces, int32_t P,
                                                         int32_t O, int32_t OB, int32_t I, int32_t G, T* x) {
-  constexpr int EL = 16;
+  constexpr int EL = 16 / (int)sizeof(T);
   const int64_t step = (int64_t)gridDim.x * kThreads;
   for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < pieces; i += step) {
     const int64_t row = (i >> 32) ? i / P : (int64_t)((uint32_t)i / (uint32_t)P);
@@ -168,39 +169,41 @@ __global__ __launch_bounds__(kThreads) void k_fp8_unpack(const uint8_t* q, const
       const int64_t mat = (row >> 32) ? row / O : (int64_t)((uint32_t)row / (uint32_t)O);
       er = mat * OB + (row - mat * O) / kFp8Block;
     }
-    const float s = fp8_scale(e[er * G + c / kFp8Block]);
     const uint8_t* src = q + row * I + c;
     T* dst = x + row * I + c;
-    v4u w{0u, 0u, 0u, 0u};
+    uint32_t w[EL / 4] = {};
     if (WHOLE || n >= EL) {
-      if constexpr (WHOLE)
-        w = __builtin_nontemporal_load(reinterpret_cast<const v4u*>(src));
-      else
-        __builtin_memcpy(&w, src, 16);
+      if constexpr (WHOLE && EL == 8) {
+        const v2u v = __builtin_nontemporal_load(reinterpret_cast<const v2u*>(src));
+        w[0] = v[0];
+        w[1] = v[1];
+      } else if constexpr (WHOLE) {
+        w[0] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(src));
+      } else {
+        __builtin_memcpy(w, src, EL);
+      }
     } else {
 #pragma unroll
       for (int k = 0; k < EL; ++k)
         if (k < n) w[k >> 2] |= (uint32_t)src[k] << (8 * (k & 3));
     }
+    const float s = fp8_scale(e[er * G + c / kFp8Block]);
     float v[EL];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) fp8_values4(w[k], s, v + 4 * k);
+    for (int k = 0; k < EL / 4; ++k) fp8_values4(w[k], s, v + 4 * k);
     if (WHOLE || n >= EL) {
+      v4u o;
 #pragma unroll
-      for (int k = 0; k < (int)sizeof(T); ++k) {
-        v4u o;
-#pragma unroll
-        for (int d = 0; d < 4; ++d) {
-          if constexpr (sizeof(T) == 4)
-            o[d] = __float_as_uint(v[4 * k + d]);
-          else
-            o[d] = bf16_pair(v[8 * k + 2 * d], v[8 * k + 2 * d + 1]);
-        }
-        if constexpr (WHOLE)
-          __builtin_nontemporal_store(o, reinterpret_cast<v4u*>(dst) + k);
+      for (int d = 0; d < 4; ++d) {
+        if constexpr (sizeof(T) == 4)
+          o[d] = __float_as_uint(v[d]);
         else
-          __builtin_memcpy(reinterpret_cast<char*>(dst) + 16 * k, &o, 16);
+          o[d] = bf16_pair(v[2 * d], v[2 * d + 1]);
       }
+      if constexpr (WHOLE)
+        __builtin_nontemporal_store(o, reinterpret_cast<v4u*>(dst));
+      else
+        __builtin_memcpy(dst, &o, 16);
     } else {
 #pragma unroll
       for (int k = 0; k < EL; ++k)
@@ -237,9 +240,10 @@ hipError_t pack(const T* x, int64_t mats, int64_t O, int32_t I, bool weights, ui
 template <typename T>
 hipError_t unpack(const uint8_t* q, const uint8_t* e, int64_t mats, int64_t O, int32_t I, bool weights, T* x,
                   hipStream_t s) {
-  const int32_t G = (I + kFp8Block - 1) / kFp8Block, P = (I + 15) / 16;
+  constexpr int EL = 16 / (int)sizeof(T);
+  const int32_t G = (I + kFp8Block - 1) / kFp8Block, P = (I + EL - 1) / EL;
   const int64_t pieces = mats * O * P;
-  const bool whole = aligned16(x) && aligned16(q) && I % 16 == 0;
+  const bool whole = aligned16(x) && aligned16(q) && I % EL == 0;
   auto* kern = whole ? k_fp8_unpack<T, true> : k_fp8_unpack<T, false>;
   const dim3 grid((unsigned)std::min<int64_t>((pieces + kThreads - 1) / kThreads, 1 << 20));
   hipLaunchKernelGGL(kern, grid, dim3(kThreads), 0, s, q, e, pieces, P, weights ? (int32_t)O : 0,
