@@ -81,8 +81,9 @@ struct Tile {
 using Big = Tile<256, 256, 4, 2, 2>;
 using Small = Tile<128, 64, 2, 2, 2>;
 using Few = Tile<128, 32, 2, 1, 2>;
-// The gated activation in 8 bits: the 128 activations that share an exponent are one tile's.  Eight waves, as one such
-// block fills a CU's LDS: 32 rows of 32 experts, 1,000 -> 2 x 333, 24 us against 30 with four.
+// The gated activation in 8 bits: the 128 activations that share an exponent are one tile's.  Small (rows that go
+// through registers or far apart): eight waves, as one such block fills a CU's LDS; 32 rows of 32 experts, 1,000 -> 2 x
+// 333, 24 us against 30 with four.
 using SmallWhole = Tile<256, 64, 4, 2, 2>;
 using FewWhole = Tile<256, 32, 4, 1, 2>;
 // The backward pass in 8 bits: two blocks a CU, one of which multiplies while the other stores; all waves load.
@@ -1511,7 +1512,7 @@ hipError_t pick_gemm(const ExpertGemm& g, int size, bool vec, hipStream_t s) {
   if constexpr (GP || GQ) {
     if (vec && g.wide) return launch_gemm<T, Small, LP, LQ, EPI, kWidePieces, GP, GQ>(g, s);
   }
-  if constexpr (EPI != kWeightGrad) {
+  if constexpr (EPI != kWeightGrad && !(sizeof(T) == 1 && EPI == kSwigluGrad)) {
     if (vec && size == kFew) return launch_gemm<T, Few, LP, LQ, EPI, kPieces, GP, GQ>(g, s);
   }
   if constexpr (EPI == kWeightGrad || sizeof(T) <= 2) {
