@@ -1551,9 +1551,21 @@ hipError_t pick_gemm(const ExpertGemm& g, int size, bool vec, hipStream_t s) {
 // matrix instructions take 16 times as long, so that a small tile's loads are
 // hidden too, and it wastes less at the end of an expert's rows and of the tile
 // list (49,146 rows 1,536 -> 1,024 of 48 experts: 1,298 us against 1,468).
+//
+// 8 bits: large tiles also have to be 3/8 of the CUs at least (half a tile added for each expert's last rows), since a
+// block of four waves multiplies 128 k of a small tile in a third of the time.  Large against small: one matrix 2,048 ->
+// 4,096, 1,024 rows (64 tiles) 26 against 17 us, 2,048 rows (128) 28 against 32; transposed, 2,048 rows (64) 47 against
+// 30, 4,096 rows (128) 47 against 54; 8 experts 1,024 -> 1,024, 512 rows each (80) 16.4 against 12.0, 1,024 rows (144)
+// 17.5 against 19.0.
+template <int COLS>
+bool fills(const ExpertGemm& g) {
+  const int64_t PT = (g.Pd + COLS - 1) / COLS;
+  return 4 * PT * (g.R / 128 + g.E) >= 3 * (int64_t)device_info().cu_count;
+}
 template <typename T>
 int tile_size(const ExpertGemm& g) {
   if (few_rows(g.R, g.E)) return kFew;
+  if (sizeof(T) == 1 && !fills<256>(g)) return kSmall;
   return sizeof(T) <= 2 && g.R / g.E >= 128 ? kBig : kSmall;
 }
 

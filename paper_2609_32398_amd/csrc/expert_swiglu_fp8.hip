@@ -18,7 +18,7 @@ namespace dol {
 // take the 64-row tile instead, whose loads are on their way together.
 hipError_t launch_expert_swiglu_fp8(const ExpertGemm& g, bool vec, hipStream_t s) {
   using namespace expert;
-  const int size = g.R / g.E >= 112 ? kBig : vec ? kFew : kSmall;
+  const int size = g.R / g.E >= 112 && fills<128>(g) ? kBig : vec ? kFew : kSmall;
   return pick_gemm<uint8_t, kInner, kInner, kSwiglu, false, true>(g, size, vec, s);
 }
 

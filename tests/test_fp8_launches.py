@@ -25,19 +25,25 @@ def _layer(N, E, k, H, F, dtype=1, w8=True):
             ["p", dtype, "p", 0, "p", 0, "p", e, "p", e, N, E, k, H, F, "p", "p", 1 << 40, None]]
 
 
-def _threads(record, call):  # noqa: F811
-    launches = [r for r in record([call]) if r[1] < 0]
-    return [r[4] for r in launches]
+def _launched(record, call):  # noqa: F811
+    """(threads, whether most of a CU's shared memory) of each launch."""
+    return [(r[4], r[2] > 100 << 10) for r in record([call]) if r[1] < 0]
 
 
 def test_the_gpu_tests_shapes_reach_their_tiles(record):  # noqa: F811
     import test_gpu_expert_fp8 as t
 
-    seen = {_threads(record, _matmul(N, N * k, E, O, I, tr))[0] for N, E, k, O, I in t.SHAPES for tr in (0, 1)}
-    assert seen == {128, 256, 512}
-    seen = {_threads(record, _swiglu(N, N * k, E, H, F))[0] for N, E, k, H, F in t.GATED}
-    assert seen == {256, 512}  # 256 x 32 by four waves; through registers 256 x 64, and 256 x 256, by eight
-    seen = {tuple(_threads(record, _grad(N, E, k, H, F))) for N, E, k, H, F in t.GATED}
+    whole = lambda *w: all(v % 16 == 0 for v in w)  # noqa: E731
+    seen = {(*_launched(record, _matmul(N, N * k, E, O, I, tr))[0], whole(O, I), tr)
+            for N, E, k, O, I in t.SHAPES for tr in (0, 1)}
+    for tr in (0, 1):
+        for pieces in (True, False):  # 128 x 64 and 256 x 256
+            assert {(256, False, pieces, tr), (512, True, pieces, tr)} <= seen
+        assert (128, False, True, tr) in seen  # 128 x 32
+    seen = {(*_launched(record, _swiglu(N, N * k, E, H, F))[0], whole(H)) for N, E, k, H, F in t.GATED}
+    # 256 x 32, through registers 256 x 64, and 256 x 256
+    assert seen == {(256, False, True), (512, False, False), (512, True, True), (512, True, False)}
+    seen = {tuple(n for n, _ in _launched(record, _grad(N, E, k, H, F))) for N, E, k, H, F in t.GATED}
     assert seen == {(256, 256)}  # 128 x 64 and 128 x 128; then the sums of p's gradient
 
 
@@ -69,7 +75,7 @@ def test_a_layer_is_two_kernels(record, N, E, k, H, F, dtype, w8):  # noqa: F811
 
 
 def test_one_matrix_needs_no_offsets(record):  # noqa: F811
-    assert len(_threads(record, _matmul(100, 100, 1, 64, 64, 0, None))) == 1
+    assert len(_launched(record, _matmul(100, 100, 1, 64, 64, 0, None))) == 1
     record([_matmul(100, 100, 2, 64, 64, 0, None)], expect=[1])
 
 

@@ -44,7 +44,8 @@ def _products(x, w, mask, k, transposed, R):
 SHAPES = [(1, 8, 2, 64, 64), (1, 128, 8, 96, 40), (3, 4, 1, 1, 1), (70, 8, 2, 33, 7), (200, 16, 4, 130, 96),
           (129, 8, 3, 200, 264), (700, 4, 2, 256, 128), (700, 4, 2, 300, 72), (1000, 3, 2, 257, 129),
           (900, 5, 2, 528, 656), (64, 256, 8, 72, 200), (2500, 2, 1, 64, 512), (300, 8, 2, 1040, 144),
-          (1500, 4, 2, 1296, 1024), (9, 4, 2, 384, 1152)]
+          (1500, 4, 2, 1296, 1024), (9, 4, 2, 384, 1152), (2600, 3, 2, 2064, 144), (2600, 3, 2, 144, 2064),
+          (2600, 3, 2, 2065, 139), (2600, 3, 2, 139, 2065)]
 
 
 @pytest.mark.parametrize("N,E,k,O,I", SHAPES)
@@ -82,7 +83,7 @@ def test_matmul_of_normal_operands(dl, N, E, k, O, I, transposed):
 
 
 @pytest.mark.parametrize("R,O,I", [(1, 1, 1), (1, 2048, 768), (5, 33, 7), (130, 256, 128), (1000, 257, 129),
-                                   (2049, 640, 1040)])
+                                   (2049, 640, 1040), (2600, 3088, 144), (2600, 144, 3089)])
 @pytest.mark.parametrize("transposed", [False, True])
 def test_one_matrix_for_all_rows(dl, R, O, I, transposed):
     print(f"[case] dense fp8 R={R} O={O} I={I} t={transposed}", flush=True)
@@ -208,7 +209,8 @@ def test_matmul_far_tokens(dl):
 # N, E, k, H, F
 GATED = [(1, 8, 2, 64, 32), (1, 128, 8, 72, 96), (5, 4, 1, 1, 1), (60, 8, 2, 40, 33), (200, 16, 4, 128, 96),
          (700, 4, 2, 144, 256), (700, 4, 2, 64, 200), (1000, 3, 2, 129, 129), (600, 3, 2, 80, 48), (64, 64, 8, 96, 160),
-         (300, 4, 2, 656, 400), (900, 3, 2, 1040, 272), (130, 4, 2, 333, 64)]
+         (300, 4, 2, 656, 400), (900, 3, 2, 1040, 272), (130, 4, 2, 333, 64), (2600, 3, 2, 272, 1168),
+         (2600, 3, 2, 267, 1171)]
 
 
 def _row_probs(p, mask, k, R):
