@@ -178,30 +178,63 @@ def test_matmul_offsets_and_tokens_out_of_range(dl):
         same(y[a:b], (v[a:b] @ m[e].t()).to(BF16), "y")
 
 
-def test_matmul_far_tokens(dl):
-    # rows taken from tokens more than 4 GiB apart, and a result past 2^31 elements' place
-    N, H, E, O = (1 << 21) + 64, 2048, 2, 64
-    gen = _gen(9)
+def _far(dl, gen, N, H, scale=0):
+    """An Fp8 of [N, H] past 4 GiB whose values lie in up to 300 rows, the first and the last among them: (a, those rows,
+    their values)."""
     q = torch.zeros(N, H, dtype=torch.uint8, device="cuda").view(E4M3)
     e = torch.full((N, H // BLOCK), 127, dtype=torch.uint8, device="cuda")
-    part = lattice(dl, gen, 300, H)
+    part = lattice(dl, gen, 300, H, scale=scale)
     at = torch.randint(0, N, (300,), generator=gen)
     at[:4] = torch.tensor([0, N - 1, N - 2, 1 << 21])
     at = at.unique()
     n = at.numel()
     q.view(torch.uint8)[at.cuda()] = part.q.view(torch.uint8)[:n]
     e[at.cuda()] = part.e[:n]
-    w = lattice(dl, gen, E, O, H, weights=True)
+    return dl.Fp8(q, e), at, values(dl.Fp8(part.q[:n], part.e[:n]))
+
+
+def _far_rows(dl, N, at):
+    """Rows of two experts that take the tokens `at` backwards, 100 for the first; no others of the N."""
     tok = torch.zeros(N, dtype=torch.int32)
-    tok[:n] = at.flip(0).int()
-    rows = dl.ExpertRows(torch.tensor([0, 100, n], dtype=torch.int32).cuda(), tok.cuda(),
-                         torch.zeros(N, 1, dtype=torch.int32).cuda(), torch.zeros(N, 1, dtype=torch.int32).cuda())
+    tok[:at.numel()] = at.flip(0).int()
+    none = torch.full((N, 1), -1, dtype=torch.int32).cuda()
+    return dl.ExpertRows(torch.tensor([0, 100, at.numel()], dtype=torch.int32).cuda(), tok.cuda(), none, none)
+
+
+def test_matmul_far_tokens(dl):
+    # rows taken from tokens more than 4 GiB apart
+    N, H, O = (1 << 21) + 64, 2048, 64
+    gen = _gen(9)
+    x, at, v = _far(dl, gen, N, H)
+    w = lattice(dl, gen, 2, O, H, weights=True)
     print("[case] matmul fp8 far tokens", flush=True)
-    y = dl.do_expert_matmul_fp8(dl.Fp8(q, e), w, rows, gather=True)
-    v = values(dl.Fp8(part.q[:n], part.e[:n])).flip(0)
-    m = values(w, True)
+    y = dl.do_expert_matmul_fp8(x, w, _far_rows(dl, N, at), gather=True)
+    v, m = v.flip(0), values(w, True)
     ref = torch.cat([v[:100] @ m[0].t(), v[100:] @ m[1].t()])
-    same(y[:n], ref.to(BF16), "y")
+    same(y[:at.numel()], ref.to(BF16), "y")
+
+
+def test_swiglu_and_its_gradient_far_tokens(dl):
+    N, H, F = (1 << 21) + 64, 2048, 48
+    gen = _gen(10)
+    x, at, v = _far(dl, gen, N, H, scale=_scale(H))
+    w1, w2 = lattice(dl, gen, 2, 2 * F, H, weights=True), lattice(dl, gen, 2, H, F, weights=True)
+    rows, n = _far_rows(dl, N, at), at.numel()
+    print("[case] swiglu fp8 far tokens", flush=True)
+    _, kept = dl.do_expert_swiglu_fp8(x, w1, rows, checkpoint=True)
+    v, m = v.flip(0), values(w1, True)
+    a = torch.cat([v[:100] @ m[0].t(), v[100:] @ m[1].t()]).view(n, 2, F)
+    q, e = _act8_ref(a)
+    same(kept.e[:n].int() - 127, e, "checkpoint's exponents")
+    same(kept.q[:n].double(), q, "checkpoint")
+    # the same tokens as gradients: du = p dh silu(g)
+    da, _, none = dl.do_expert_swiglu_grad_fp8(x, w2, rows, kept)
+    assert none is None
+    m = values(w2, True)
+    dh = torch.cat([v[:100] @ m[0], v[100:] @ m[1]])
+    g = q[:, 0] * power(e)[:, 0].repeat_interleave(32, 1)[:, :F]
+    ref = dh * g * torch.sigmoid(g)
+    within(da[:n, F:], ref, ref.abs() * ((g.abs() + 8) * 4 * EPS32 + 8 * EPS32 + 1.01 * EPS16) + 1e-30, "du")
 
 
 # --- the gated activation --------------------------------------------------------------------------------------------
