@@ -993,8 +993,9 @@ def do_expert_layer(x: torch.Tensor, scores: torch.Tensor, k: int, w1, w2, p: to
     if isinstance(w1, Fp8) != isinstance(w2, Fp8):
         raise ValueError("w1 and w2 must both be Fp8 or both tensors")
     if isinstance(w1, Fp8):
-        F2, _ = _fp8_weights(w1, "w1", E)
-        F = F2 // 2
+        if not isinstance(w1.q, torch.Tensor) or w1.q.dim() != 3:
+            raise ValueError(f"w1 must be an Fp8 of shape [{E}, 2 F, {H}] (do_fp8_pack with weights=True)")
+        F = w1.q.shape[1] // 2
         _want_fp8(w1, "w1", (E, 2 * F, H), True)
         _want_fp8(w2, "w2", (E, H, F), True)
         ptrs = (w1.q.data_ptr(), w1.e.data_ptr(), w2.q.data_ptr(), w2.e.data_ptr())

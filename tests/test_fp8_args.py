@@ -104,3 +104,29 @@ def test_binding(dl):
     _refused(dl.do_expert_layer, torch.zeros(2, 64), torch.zeros(2, 4), 2, w1, w2, say="device tensor")
     _refused(dl.do_expert_swiglu_fp8, _fp8(dl, 10, 64), torch.zeros(4, 32, 64), rows)
     _refused(dl.do_expert_swiglu_grad_fp8, _fp8(dl, 10, 64), torch.zeros(4, 64, 32), rows, None)
+
+
+@pytest.mark.gpu
+def test_layer_binding_on_the_device(dl):
+    # what is looked at behind the tokens' and the scores' device
+    x, s = torch.zeros(2, 64, device="cuda"), torch.zeros(2, 4, device="cuda")
+    w1, w2 = torch.zeros(4, 16, 64, device="cuda"), torch.zeros(4, 64, 8, device="cuda")
+    q1, q2 = dl.do_fp8_pack(w1, True), dl.do_fp8_pack(w2, True)
+    f = dl.do_expert_layer
+    _refused(f, x, s, 0, w1, w2, say="k = 0")
+    _refused(f, x, s, 5, w1, w2, say="k = 5")
+    _refused(f, x, s[:1], 2, w1, w2, say="scores")
+    _refused(f, x, s.double(), 2, w1, w2, say="dtype")
+    _refused(f, x, s, 2, w1, q2, say="both")
+    _refused(f, x, s, 2, w1[:, :15].contiguous(), w2, say="w1")
+    _refused(f, x, s, 2, w1, w2.bfloat16(), say="dtype")
+    _refused(f, x, s, 2, w1, w2.transpose(1, 2), say="w2")
+    _refused(f, x, s, 2, q1, dl.Fp8(q2.q, q2.e[:, :, :0].contiguous()), say="w2.e")
+    _refused(f, x, s, 2, dl.Fp8(None, None), q2, say="w1")
+    _refused(f, x, s, 2, dl.Fp8(q1.q.view(torch.uint8), q1.e), q2, say="w1.q")
+    _refused(f, x, s, 2, w1, w2, torch.zeros(2, 5, device="cuda"), say="p has shape")
+    _refused(f, x, s, 2, w1, w2, out=torch.zeros(2, 64, device="cuda", dtype=torch.bfloat16), say="out")
+    _refused(dl.do_expert_matmul_fp8, dl.do_fp8_pack(x), q1, None, say="[1, O, I]")
+    _refused(dl.do_expert_matmul_fp8, dl.do_fp8_pack(x), dl.Fp8(q1.q[:1], q1.e[:1]), None, transposed=True, say="x.q")
+    _refused(dl.do_fp8_unpack, dl.Fp8(q1.q, q1.e[:, :, :0].contiguous()), torch.float32, say="e has shape")
+    torch.cuda.synchronize()
