@@ -474,7 +474,7 @@ __global__ __launch_bounds__(kDownWaves* kWave, kOccupancy<NT>) void k_layer_dow
   }
   if (S == 1) return;
   // The parts are stored and loaded past the L2 caches, which belong to an XCD each, so that they only have to be
-  // done before the count: a fence would write a whole cache back (60 us more).
+  // done before the count: a fence would write a whole cache back (60 to 80 us more).
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   if (tid == 0)
