@@ -564,8 +564,8 @@ do_status do_expert_layer(const void* x, do_dtype dtype, const void* scores, do_
  * The third adds an input check.  NaN scores have a defined rank (below -inf,
  * equal to each other), so results are defined without it:
  *   DO_OPT_CHECK_FINITE  0 (default) off; 1: do_topk_signature, do_fused,
- *                        do_stream_append and do_stream_append_many first scan
- *                        their scores for NaN (+-inf are ordinary values), wait
+ *                        do_stream_append, do_stream_append_many and
+ *                        do_expert_layer first scan their scores for NaN (+-inf are ordinary values), wait
  *                        for the scan on the caller's stream, and return
  *                        DO_ERR_NONFINITE without writing anything (the
  *                        stream handle is unchanged) if one is found.  Such a

@@ -187,6 +187,10 @@ do_status check_finite(const void* const* xs, int32_t count, int64_t elems_each,
 
 }  // namespace
 
+do_status dol::check_finite_scores(const void* scores, int64_t n, do_dtype dt, hipStream_t s) {
+  return check_finite(&scores, 1, n, dt, s);
+}
+
 // Copies of a stream's co-occurrence counters (block b of an append adds its
 // counts into copy b % kStreamCopies).  Eight copies, one per XCD, were
 // measured: the append kernel took the same time at workload 3 and the

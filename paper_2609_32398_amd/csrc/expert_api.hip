@@ -549,6 +549,7 @@ DOLOSS_API do_status do_expert_layer(const void* x, do_dtype dtype, const void* 
   DO_TRY(check_ptr(workspace, 16, "workspace is NULL or not 16-byte aligned"));
   if (workspace_bytes < do_expert_layer_workspace(dtype, N, E, k, H, F))
     return set_error(DO_ERR_INVALID_ARG, "workspace is smaller than do_expert_layer_workspace(dtype, N, E, k, H, F)");
+  DO_TRY(dol::check_finite_scores(scores, N * E, scores_dtype, stream));
   dol::LayerArgs a{};
   a.x = x;
   a.scores = scores;

@@ -16,6 +16,9 @@ constexpr int64_t kMaxRows = (int64_t(1) << 31) - 1024;
 // do_last_error of the calling thread, and the status itself.
 do_status set_error(do_status st, const char* msg);
 
+// The check-finite mode's scan of n scores (DO_OK where the mode is off).
+do_status check_finite_scores(const void* scores, int64_t n, do_dtype dt, hipStream_t s);
+
 // 512-token units are the work items of the row kernels; at most kRowChunks
 // blocks take a contiguous range of them each.
 constexpr int64_t kRowChunks = 512;

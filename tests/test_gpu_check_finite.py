@@ -134,3 +134,63 @@ def test_check_mode_refuses_stream_capture(dl, syn, check_mode):
         with pytest.raises(dl.DoLossError) as ei:
             dl.do_fused(xd, k, bits=bits, D=D, out=out)
     assert ei.value.status == dl.DO_ERR_INVALID_ARG
+
+
+def _layer(dl, sdtype, w8, offset=0):
+    """Arguments of do_expert_layer whose scores start `offset` elements past an aligned address."""
+    g = torch.Generator()
+    g.manual_seed(940)
+    N, E, k, H, F = 13, 40, 5, 72, 24
+    scores = torch.empty(N * E + offset, dtype=sdtype, device="cuda")[offset:].view(N, E)
+    scores.copy_(torch.randn(N, E, generator=g))
+    x = torch.randn(N, H, generator=g).bfloat16().cuda()
+    w1 = torch.randn(E, 2 * F, H, generator=g).bfloat16().cuda()
+    w2 = torch.randn(E, H, F, generator=g).bfloat16().cuda()
+    if w8:
+        w1, w2 = dl.do_fp8_pack(w1, weights=True), dl.do_fp8_pack(w2, weights=True)
+    return x, scores, k, w1, w2
+
+
+@pytest.mark.parametrize("sdtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("offset", [0, 1])
+@pytest.mark.parametrize("w8", [False, True])
+def test_layer_reports_a_nan_score_and_writes_nothing(dl, check_mode, sdtype, offset, w8):
+    x, scores, k, w1, w2 = _layer(dl, sdtype, w8, offset)
+    out = torch.full_like(x, 7.0)
+    for pos in (0, scores.numel() // 2 + 3, scores.numel() - 1):
+        print(f"[case] check-finite layer {sdtype} offset={offset} w8={w8} pos={pos}", flush=True)
+        was = scores.view(-1)[pos].clone()
+        scores.view(-1)[pos] = float("nan")
+        with pytest.raises(dl.DoLossError) as ei:
+            dl.do_expert_layer(x, scores, k, w1, w2, out=out)
+        assert ei.value.status == dl.DO_ERR_NONFINITE
+        torch.cuda.synchronize()
+        assert bool((out == 7.0).all()), "the output was written"
+        scores.view(-1)[pos] = was
+    # the scores alone are looked at: NaN elsewhere is computed with
+    x[2, 1] = float("nan")
+    assert dl.do_expert_layer(x, scores, k, w1, w2, out=out)[2].isnan().all()
+
+
+@pytest.mark.parametrize("sdtype", [torch.float32, torch.bfloat16])
+def test_layer_with_infinities_is_the_unchecked_call(dl, sdtype):
+    x, scores, k, w1, w2 = _layer(dl, sdtype, False)
+    scores[0, 3], scores[5], scores[12, 39] = float("inf"), float("-inf"), float("-inf")
+    ref = dl.do_expert_layer(x, scores, k, w1, w2)
+    dl.set_option(dl.DO_OPT_CHECK_FINITE, 1)
+    try:
+        got = dl.do_expert_layer(x, scores, k, w1, w2)
+    finally:
+        dl.set_option(dl.DO_OPT_CHECK_FINITE, 0)
+    assert torch.equal(got, ref)
+
+
+def test_check_mode_refuses_a_captured_layer(dl, check_mode):
+    x, scores, k, w1, w2 = _layer(dl, torch.float32, False)
+    out = dl.do_expert_layer(x, scores, k, w1, w2)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        with pytest.raises(dl.DoLossError) as ei:
+            dl.do_expert_layer(x, scores, k, w1, w2, out=out)
+    assert ei.value.status == dl.DO_ERR_INVALID_ARG
