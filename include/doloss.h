@@ -508,7 +508,13 @@ do_status do_fp8_unpack_weights(const uint8_t* q, const uint8_t* e, int64_t mats
  * bits; an operand's block that reads as NaN gives NaN.
  *   do_expert_matmul_fp8       y is bf16.  offsets may be NULL with E = 1: then
  *                              the expert has all R rows
- *   do_expert_swiglu_fp8       h is packed again, [R][F] with h_exp [R][ceil(F / 128)]
+ *   do_expert_swiglu_fp8       h is packed again, [R][F] with h_exp [R][ceil(F / 128)].
+ *                              What the matrix instructions drop (about 1e-5 of a
+ *                              sum of normal operands) can carry a value that
+ *                              lies that near to a border to the neighbouring
+ *                              e4m3 value: h as a whole is then about 1e-3 in
+ *                              norm from the packing of exact sums, beside the
+ *                              2e-2 or more that packing itself costs
  *   do_expert_swiglu_grad_fp8  da and h are bf16; workspace and dp as in
  *                              do_expert_swiglu_grad
  */
@@ -540,7 +546,12 @@ do_status do_expert_swiglu_grad_fp8(const uint8_t* dy, const uint8_t* dy_exp, co
  *           overlap in time share one
  * Products, sums and activations are computed in fp32, the activations between
  * the products rounded to dtype; a token's sum is taken in an order that the
- * call's sizes and choices fix.
+ * call's sizes and choices fix.  With weights in 8 bits x and the activations
+ * stay in dtype, where do_expert_swiglu_fp8 and do_expert_matmul_fp8 pack them:
+ * a token's output here and there differs by about 5e-2 in norm.  For more
+ * tokens do_fp8_unpack_weights and the calls in dtype give these values but for
+ * roundings.  The ranking takes a round for each of k: 0.2 us of 128 experts (64
+ * tokens 0.85), 10 us of 1,024 experts with 64 tokens.
  */
 int64_t do_expert_layer_workspace(do_dtype dtype, int64_t N, int32_t E, int32_t k, int32_t H, int32_t F);
 do_status do_expert_layer(const void* x, do_dtype dtype, const void* scores, do_dtype scores_dtype, const void* p,

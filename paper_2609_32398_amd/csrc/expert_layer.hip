@@ -6,18 +6,23 @@
 // tokens' values beside them; a lane's 16 bytes are one, two or four instructions' k, in the same order for both
 // operands.  Weights in 8 bits become bf16 (or fp32) with their power of two in registers, exactly.
 //
-//   k_layer_up    Every block finds the k best experts of all tokens (3 us for one token of 128 experts, 4 for 16) and,
-//                 as N <= 64, holds an expert's tokens as one word of 64 bits.  Its tiles are 8 activations of an
+//   k_layer_up    Every block finds the k best experts of all tokens and, as N <= 64, holds an expert's tokens as one
+//                 word of 64 bits.  The kernel without weights to speak of (64 and 8 wide) takes 4.2 us for the best of
+//                 128 experts and 6.6 for the best 8, of one token and of 16; each further round 0.2 us (64 tokens
+//                 0.85).  From 257 experts on a wave takes a token: 8 of 1,024 experts 11 us, of 64 tokens 91, and
+//                 about 10 ms where 64 tokens take all 1,024.  Its tiles are 8 activations of an
 //                 expert: their 8 gate and 8 up rows are the 16 rows of an instruction, its four waves take a quarter
 //                 of H each.
 //   k_layer_down  A block takes 16 columns of y and a share of the chosen experts: its waves take the experts in turn
 //                 and add their tokens' sums in LDS, each wave in a place of its own, so that the order of a sum is
 //                 fixed; the blocks of a column tile meet through memory.
 //
-// One token, 8 of 128 experts, 2,048 and 768 wide, bf16: 15 + 9 us, where the 76 MB of weights take 16 at the rate of
-// a copy; the rest is the ranking, two launches and the blocks' meeting.  16 tokens, 8 bits: 60 + 34 us (390 MB, 4.1
-// TB/s): waves that read more than others at the kernels' ends.  37 tokens of 6 of 64 experts, 1,000 and 333 wide, fp32:
-// 43 + 28 us (245 MB, 3.5 TB/s), whose rows begin at any 4 bytes.
+// One token, 8 of 128 experts, 2,048 and 768 wide, bf16: 15.4 + 9.1 us, 6.6 + 3.8 of them without weights to speak of,
+// so the 50 and 25 MB of weights come at 5.7 and 4.8 TB/s (reading 76 MB alone: 5.3).  16 tokens, 8 bits: 60 + 34 us
+// (78 experts' 245 and 123 MB, 4.1 and 3.6 TB/s): waves that read more than others at the kernels' ends.  37 tokens of
+// 6 of 48 experts, 1,000 and 333 wide, fp32: 40 to 43 + 27 to 28 us (128 and 64 MB, 3.0 and 2.3 TB/s).  Their rows are
+// no multiples of 64 bytes, so that neighbours share pieces of a line (159 and 86 MB counted; 1,008 and 336 wide 147
+// and 78 MB, 35 + 23 us).
 #include <algorithm>
 #include <atomic>
 #include <type_traits>
@@ -52,7 +57,10 @@ struct Form {
   static constexpr int piece = 4 * W;                      // k of four lanes' pieces
   static constexpr int step = P * piece;
   using Element = std::conditional_t<W8, uint8_t, T>;
-  // steps that are on their way together, for NT tiles of activations: as many as leave four waves a SIMD
+  // steps that are on their way together, for NT tiles of activations: as many as leave four waves a SIMD, two at least.
+  // Two of fp32 activations beside 8-bit weights do not fit: 8 to 21 registers spill with one tile, 61 to 65 with two
+  // (16 tokens 162 us against 92 in bf16, 64 tokens 334 against 176, the fp32 matrix instructions included).  bf16 beside
+  // 8-bit weights spills 2 in the first kernel of two tiles, nothing else does.
   template <int NT>
   static constexpr int ahead = std::max(2, std::min(8, 68 / (P * (4 + 4 * X * NT))));
 

@@ -1,10 +1,14 @@
 // Products of rows with their expert's weights, and with the transposed weights, in 8-bit floating point.
 //
 // 524,288 rows of 128 experts, 768 -> 2,048: 1,010 us, 1,630 TFLOP/s (the library on one product of this width:
-// 1,660).  8,191 rows 2,048 -> 4,096: 64 us, 2,160 TFLOP/s (the library at 8,192^3: 2,650).  49,146 rows of 48 experts,
-// 1,536 -> 1,024 transposed: 98 us, 1,580 TFLOP/s, of which a fifth is the last round of its 864 tiles.  64 tokens of 8
-// of 128 experts, 768 -> 2,048: 40 us, the weights at 5.0 TB/s.  Bound by the operands' way to LDS (a stage of 64 KiB
-// and its products take 3,500 cycles, the products alone 2,048) and, at 768, by 5,300 cycles of outputs a tile.
+// 1,660).  8,191 rows 2,048 -> 4,096: 64 us, 2,160 TFLOP/s (the library at 8,192^3: 2,650).  49,146 rows of 48
+// experts, 1,536 -> 1,024 transposed: 98 us, 1,580 TFLOP/s, of which a fifth is the last round of its 864 tiles.  64
+// tokens of 8 of 128 experts, 768 -> 2,048: 40 us, the weights at 5.0 TB/s.  524,288 rows taken from 65,536 tokens,
+// 768 -> 2,048: 931 us where rows of their own take 989, since the 50 MB of tokens stay in the caches.  One matrix,
+// 8,191 rows 4,096 -> 2,048 transposed: 61 us, 32,768 rows 224 us, 2,450 TFLOP/s (2,048 -> 4,096: 245).  Bound by the
+// operands' way to LDS (a stage of 64 KiB and its products take 3,500 cycles, the products alone 2,048) and, at 768,
+// by 5,300 cycles of outputs a tile.  Rows that go through registers (odd widths) spill 20 to 29 registers in the 256
+// x 256 tiles, the transposed one with rows by token 6; 65,536 rows 1,003 -> 1,501: 331 us, 1,008 -> 1,504: 156.
 #include <algorithm>
 
 #include "expert_gemm.h"

@@ -13,9 +13,14 @@
 namespace dol {
 
 // The 32-row tile up to 112 rows an expert on average, since one with 64 rows of 256 fills a CU's LDS by itself: 8 of
-// 64 experts a token, 2,048 -> 2 x 768, 32 rows against 256: 64 rows an expert 57 against 73 us (the 64-row tile 75), 96
-// rows 71 against 75 (73), 128 rows 89 against 77 (92), 256 rows 143 against 116 (144).  Rows that go through registers
-// take the 64-row tile instead, whose loads are on their way together.
+// 64 experts a token, 2,048 -> 2 x 768, 32 rows against 256: 64 rows an expert 57 against 73 us (the 64-row tile 75),
+// 96 rows 71 against 75 (73), 128 rows 89 against 77 (92), 256 rows 143 against 116 (144).  Rows that go through
+// registers take the 64-row tile instead, whose loads are on their way together (their 256-row tile spills 14
+// registers). However many rows an expert has, the large tiles also have to be 3/8 of the CUs, as fills() counts them,
+// since one takes 27 us whether others run or not.  32 rows against 256 at 2,048 in the contraction, by large tiles
+// over all experts: 1 to 48 of them 13 to 18 against 27 to 28 us, 64 (8 experts of 2,048 rows, 2 x 128) 31 against 29,
+// 96 (one of 4,096, 2 x 768) 30 against 28, 128 (8 of 2,048, 2 x 256) 44 against 30, 192 58 against 33; 64 that are
+// half empty (64 experts of 128 rows, 2 x 128) 18 against 29.
 hipError_t launch_expert_swiglu_fp8(const ExpertGemm& g, bool vec, hipStream_t s) {
   using namespace expert;
   const int size = g.R / g.E >= 112 && fills<128>(g) ? kBig : vec ? kFew : kSmall;
