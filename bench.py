@@ -108,11 +108,15 @@ def _code_only(text: str, py: bool) -> str:
 
 
 def kernel_source_digest() -> str:
-    """sha256 over the code of KERNEL_SOURCES (comments and blank lines removed)."""
+    """sha256 over the code of KERNEL_SOURCES: comments, blank lines and the list of the library's files removed (another
+    file beside the kernel does not change it)."""
     h = hashlib.sha256()
     for p in KERNEL_SOURCES:
         with open(os.path.join(ROOT, p), encoding="utf-8") as f:
-            h.update(_code_only(f.read(), p.endswith(".py")).encode())
+            text = f.read()
+        if p.endswith(".py"):
+            text = re.sub(r"(?m)^SOURCES = \[[^\]]*\]", "", text)
+        h.update(_code_only(text, p.endswith(".py")).encode())
     return h.hexdigest()
 
 
